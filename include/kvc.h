@@ -364,6 +364,22 @@ kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k
                         const double* inv_freq, void* q, void* k, void* v, void* stream);
 
 /*
+ * kvc_qkv_norm_rope: kvc_qkv_rope for models that normalise every query and
+ * key head before the rotation.  Each head x of n_q_heads and n_k_heads first
+ * becomes
+ *   x / sqrt(mean_e x[e]^2 + eps) * gamma,
+ * gamma = gamma_q or gamma_k (device bf16 [D]; one that no head uses may be
+ * NULL), eps >= 0 (an all-zero head with eps = 0 gives NaN, as the formula
+ * does), and is then rotated; float32 throughout, the angle reduced in
+ * float64, rounded once to bfloat16.  Everything else as kvc_qkv_rope; q, k, v
+ * must not overlap gamma_q or gamma_k either.
+ */
+kvc_status kvc_qkv_norm_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads,
+                             int32_t n_v_heads, int32_t head_dim, const void* gamma_q, const void* gamma_k,
+                             float eps, const int32_t* pos, double rope_theta, const double* inv_freq,
+                             void* q, void* k, void* v, void* stream);
+
+/*
  * kvc_swiglu: gated SiLU of the feed-forward block.
  *   out[i,c] = silu(gu[i,c]) * gu[i, inter + c],  silu(g) = g / (1 + e^-g),
  * in float32 (hardware exponential and reciprocal, a few float32 ulps) and
@@ -443,6 +459,100 @@ kvc_status kvc_stage_layers(const kvc_layout* L, const kvc_plan* plan, int32_t n
                             const void* const* k_chunks, const void* const* v_chunks,
                             void* const* k_cache, void* const* v_cache, void* const* events,
                             void* stream);
+
+/*
+ * Pages: the rows that sequences add behind a shared context (generated
+ * tokens, a question of their own), in pages of a pool, so that sequences
+ * grow, end, continue each other and share rows without their rows moving.
+ * A pool's keys and values are device bf16 [n_layers, n_pages, page_rows, Hkv,
+ * D] each; one set of tables (host struct, device arrays, the caller's) serves
+ * every layer:
+ *   len[s]: rows of slot s; row r is row r % page_rows of page
+ *   table[s, r / page_rows].  Entries of the table from ceil(len / page_rows)
+ *   on mean nothing and are neither read nor written.
+ *   ref[p]: how many table entries hold page p; 0: the page is free.
+ * A fresh pool has len and ref all zero.  A len outside [0, max_pages x
+ * page_rows] is taken as the nearer end; table entries outside [0, n_pages)
+ * count for no page.  page_rows: a power of two in [8, 1024]
+ * (KVC_ERR_UNSUPPORTED otherwise); n_pages >= 1; at most KVC_PAGES_MAX_SLOTS
+ * slots; n_pages x page_rows and max_pages x page_rows at most 2^31 - 128.
+ * Results follow from the tables alone (free pages from the lowest number up,
+ * slots in order).  The slot arrays keep, src_of and n_new are dense, one entry
+ * per slot, so no slot can be named twice.
+ */
+#define KVC_PAGES_MAX_SLOTS 65536
+typedef struct kvc_pages {
+  int32_t n_pages;
+  int32_t page_rows;
+  int32_t n_slots;
+  int32_t max_pages; /* table entries per slot */
+  int32_t* ref;      /* device [n_pages] */
+  int32_t* table;    /* device [n_slots, max_pages] */
+  int32_t* len;      /* device [n_slots] */
+} kvc_pages;
+
+/* Scratch that kvc_pages_fork, _reserve and _compact need (16-byte aligned;
+ * it needs no initialisation and holds nothing useful afterwards). */
+kvc_status kvc_pages_workspace(const kvc_pages* P, size_t* bytes);
+
+/*
+ * kvc_pages_trim: slot s keeps its first keep[s] rows (keep[s] < 0, or not
+ * below len[s]: all of them) and lets go of the pages behind them: 0 ends a
+ * sequence, len[s] - n takes n rows back.  keep: device int32 [n_slots].
+ */
+kvc_status kvc_pages_trim(const kvc_pages* P, const int32_t* keep, void* stream);
+
+/*
+ * kvc_pages_fork: every slot s with src_of[s] in [0, n_slots), src_of[s] != s,
+ * lets go of its own pages and continues slot src_of[s]: it takes that slot's
+ * length and holds the same pages, as they were before the call (so slots may
+ * be exchanged).  Other slots stay.  src_of: device int32 [n_slots].  No rows
+ * are copied; kvc_pages_reserve does that for a page that is written to.
+ */
+kvc_status kvc_pages_fork(const kvc_pages* P, const int32_t* src_of, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * kvc_pages_reserve: room for n_new[s] more rows in slot s (device int32
+ * [n_slots], taken as at least 0 and at most max_new; max_new >= 1).  len grows,
+ * and rows[s, t] (device int32 [n_slots, max_new]) is the pool row (page x
+ * page_rows + row) of new row t, -1 for t >= n_new[s]: the row list that
+ * kvc_scatter_rows takes, with n_rows = n_pages x page_rows, to write a layer's
+ * keys and values.  A slot whose next row falls into a partly filled page that
+ * other slots hold gets a page of its own in its place, and copy_src[s],
+ * copy_dst[s] (device int32 [n_slots]) name the two for kvc_pages_copy, which
+ * the caller runs for every layer before writing rows; -1 where nothing is to
+ * be copied.  Slots that write to the same page take their turns in slot order,
+ * the last holder keeps it.
+ * shortage (device int32 [2]): pages missing, and slots whose table is too
+ * small.  If either is not zero the call has changed nothing: rows, copy_src
+ * and copy_dst are all -1.
+ */
+kvc_status kvc_pages_reserve(const kvc_pages* P, const int32_t* n_new, int32_t max_new, int32_t* rows,
+                             int32_t* copy_src, int32_t* copy_dst, int32_t* shortage, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/*
+ * kvc_pages_compact: renumbers the pages so that the L live ones (ref > 0) are
+ * pages 0 .. L-1, moving only those numbered L or more, in ascending order into
+ * the free pages below L in ascending order.  Tables and counts are updated;
+ * move_src[i] -> move_dst[i] (device int32 [n_pages / 2], -1 behind the last)
+ * is for kvc_pages_copy, for every layer, before anything else reads or writes
+ * the pool.  counts (device int32 [2]): L and the number of moves.
+ */
+kvc_status kvc_pages_compact(const kvc_pages* P, int32_t* move_src, int32_t* move_dst, int32_t* counts,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * kvc_pages_copy: copies page src[i] to page dst[i] in all n_layers of both
+ * pools, for i < n_pairs, or i < min(n_pairs, *count) with count non-NULL
+ * (device int32, e.g. counts + 1 of kvc_pages_compact).  Pairs with a page
+ * outside [0, n_pages) are skipped.  A page may be the source of several pairs,
+ * but one that is a destination must be in no other pair (undefined which
+ * wins).  P gives n_pages and page_rows; its device arrays are not used.
+ */
+kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t* dst, int64_t n_pairs,
+                          const int32_t* count, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
+                          void* k_pages, void* v_pages, void* stream);
 
 #ifdef __cplusplus
 }

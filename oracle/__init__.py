@@ -18,11 +18,12 @@ Modules (each function cites the passage it follows):
 * ``layer``     -- the decoder-layer steps around the attention for the
                    selected tokens: RMS normalisation, Q/K/V split with RoPE,
                    gated SiLU, the projections, and the whole layer composed
+* ``pages``     -- the page tables of sequences that grow behind the context
 
 Every function here is pinned by ``tests/test_oracle_*.py`` against closed
 forms, invariants, brute force or independent library routines.
 """
-from . import bf16, rope, deviation, select, attention, blend, layer  # noqa: F401
+from . import bf16, rope, deviation, select, attention, blend, layer, pages  # noqa: F401
 from .bf16 import bf16_to_f64, f64_to_bf16
 from .rope import inv_freq, rope_rotate, chunk_row0, chunk_delta, rope_shift
 from .deviation import key_deviation
@@ -30,10 +31,12 @@ from .select import recompute_count, select_topk, selection
 from .attention import sparse_query_attention, causal_attention
 from .blend import blend_prefill_layer
 from .layer import rms_norm, qkv_rope, swiglu, projection, decoder_layer
+from .pages import PageTables
 
 __all__ = [
     "bf16_to_f64", "f64_to_bf16", "inv_freq", "rope_rotate", "chunk_row0",
     "chunk_delta", "rope_shift", "key_deviation", "recompute_count",
     "select_topk", "selection", "sparse_query_attention", "causal_attention",
     "blend_prefill_layer", "rms_norm", "qkv_rope", "swiglu", "projection", "decoder_layer",
+    "PageTables",
 ]

@@ -52,7 +52,13 @@ class kvc_plan(ctypes.Structure):
     _fields_ = [("device", _vp), ("bytes", _sz), ("layout_id", ctypes.c_uint64)]
 
 
+class kvc_pages(ctypes.Structure):
+    _fields_ = [("n_pages", _i32), ("page_rows", _i32), ("n_slots", _i32), ("max_pages", _i32),
+                ("ref", _vp), ("table", _vp), ("len", _vp)]
+
+
 _LP = ctypes.POINTER(kvc_layout)
+_PGP = ctypes.POINTER(kvc_pages)
 _PLP = ctypes.POINTER(kvc_plan)
 _PP = ctypes.POINTER(_vp)
 _SIGS = {
@@ -79,10 +85,18 @@ _SIGS = {
     "kvc_rms_norm": (_i32, [_vp, _i64, _vp, _i64, _i32, _vp, _f32, _vp, _vp, _vp]),
     "kvc_qkv_rope": (_i32, [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _f64, ctypes.POINTER(_f64), _vp,
                             _vp, _vp, _vp]),
+    "kvc_qkv_norm_rope": (_i32, [_vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _f64,
+                                 ctypes.POINTER(_f64), _vp, _vp, _vp, _vp]),
     "kvc_swiglu": (_i32, [_vp, _i64, _i64, _vp, _vp]),
     "kvc_projection": (_i32, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp]),
     "kvc_stage_layer": (_i32, [_LP, _PLP, _PP, _PP, _vp, _vp, _vp]),
     "kvc_stage_layers": (_i32, [_LP, _PLP, _i32, _PP, _PP, _PP, _PP, _PP, _vp]),
+    "kvc_pages_workspace": (_i32, [_PGP, ctypes.POINTER(_sz)]),
+    "kvc_pages_trim": (_i32, [_PGP, _vp, _vp]),
+    "kvc_pages_fork": (_i32, [_PGP, _vp, _vp, _sz, _vp]),
+    "kvc_pages_reserve": (_i32, [_PGP, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "kvc_pages_compact": (_i32, [_PGP, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "kvc_pages_copy": (_i32, [_PGP, _vp, _vp, _i64, _vp, _i32, _i32, _i32, _vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -301,6 +315,16 @@ def kvc_qkv_rope(y, n, n_q_heads, n_k_heads, n_v_heads, head_dim, pos, rope_thet
                              _ptr(q), _ptr(k), _ptr(v), _stream(stream)))
 
 
+def kvc_qkv_norm_rope(y, n, n_q_heads, n_k_heads, n_v_heads, head_dim, gamma_q, gamma_k, eps, pos, rope_theta, q, k,
+                      v, inv_freq=None, stream=None):
+    """inv_freq: None or a sequence of head_dim/2 floats (host)."""
+    f = None if inv_freq is None else (_f64 * len(inv_freq))(*[float(x) for x in inv_freq])
+    _check(_lib.kvc_qkv_norm_rope(_ptr(y), int(n), int(n_q_heads), int(n_k_heads), int(n_v_heads), int(head_dim),
+                                  _ptr(gamma_q), _ptr(gamma_k), float(eps), _ptr(pos), float(rope_theta),
+                                  None if f is None else ctypes.cast(f, ctypes.POINTER(_f64)),
+                                  _ptr(q), _ptr(k), _ptr(v), _stream(stream)))
+
+
 def kvc_swiglu(gate_up, n, inter, out, stream=None):
     _check(_lib.kvc_swiglu(_ptr(gate_up), int(n), int(inter), _ptr(out), _stream(stream)))
 
@@ -335,4 +359,51 @@ def kvc_stage_layers(layout, plan, n_layers, k_chunks, v_chunks, k_cache, v_cach
                                  _ptrs(k_cache), _ptrs(v_cache), _ptrs(ev), _stream(stream)))
 
 
-__all__ = [n for n in _SIGS] + ["Layout", "Plan", "KvcError", "LIB_PATH", "kvc_layout", "kvc_plan"]
+class Pages:
+    """A ``kvc_pages`` (see include/kvc.h) plus references to its device arrays."""
+
+    def __init__(self, n_pages, page_rows, n_slots, max_pages, ref, table, len):
+        self.n_pages, self.page_rows = int(n_pages), int(page_rows)
+        self.n_slots, self.max_pages = int(n_slots), int(max_pages)
+        self.ref, self.table, self.len = ref, table, len
+        self.struct = kvc_pages(self.n_pages, self.page_rows, self.n_slots, self.max_pages, _ptr(ref), _ptr(table),
+                                _ptr(len))
+
+    def byref(self):
+        return ctypes.byref(self.struct)
+
+
+def _pgref(pages):
+    return None if pages is None else pages.byref()
+
+
+def kvc_pages_workspace(pages) -> int:
+    b = _sz(0)
+    _check(_lib.kvc_pages_workspace(_pgref(pages), ctypes.byref(b)))
+    return b.value
+
+
+def kvc_pages_trim(pages, keep, stream=None):
+    _check(_lib.kvc_pages_trim(_pgref(pages), _ptr(keep), _stream(stream)))
+
+
+def kvc_pages_fork(pages, src_of, ws, ws_bytes, stream=None):
+    _check(_lib.kvc_pages_fork(_pgref(pages), _ptr(src_of), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def kvc_pages_reserve(pages, n_new, max_new, rows, copy_src, copy_dst, shortage, ws, ws_bytes, stream=None):
+    _check(_lib.kvc_pages_reserve(_pgref(pages), _ptr(n_new), int(max_new), _ptr(rows), _ptr(copy_src),
+                                  _ptr(copy_dst), _ptr(shortage), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def kvc_pages_compact(pages, move_src, move_dst, counts, ws, ws_bytes, stream=None):
+    _check(_lib.kvc_pages_compact(_pgref(pages), _ptr(move_src), _ptr(move_dst), _ptr(counts), _ptr(ws),
+                                  int(ws_bytes), _stream(stream)))
+
+
+def kvc_pages_copy(pages, src, dst, n_pairs, count, n_layers, n_kv_heads, head_dim, k_pages, v_pages, stream=None):
+    _check(_lib.kvc_pages_copy(_pgref(pages), _ptr(src), _ptr(dst), int(n_pairs), _ptr(count), int(n_layers),
+                               int(n_kv_heads), int(head_dim), _ptr(k_pages), _ptr(v_pages), _stream(stream)))
+
+
+__all__ = [n for n in _SIGS] + ["Layout", "Plan", "KvcError", "LIB_PATH", "kvc_layout", "kvc_plan", "Pages", "kvc_pages"]

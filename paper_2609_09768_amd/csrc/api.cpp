@@ -848,10 +848,10 @@ kvc_status kvc_rms_norm(const void* x, int64_t n_x_rows, const int32_t* rows, in
   return ok();
 }
 
-kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads, int32_t n_v_heads,
-                        int32_t head_dim, const int32_t* pos, double rope_theta, const double* inv_freq,
-                        void* q, void* k, void* v, void* stream) {
-  const char* W = "kvc_qkv_rope";
+// kvc_qkv_rope, and with norm the form that normalises the heads first.
+static kvc_status qkv_rope_impl(const char* W, const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads,
+                                int32_t n_v_heads, int32_t head_dim, const kvc::HeadNorm* norm, const int32_t* pos,
+                                double rope_theta, const double* inv_freq, void* q, void* k, void* v, void* stream) {
   if (n < 0 || n > kMaxRows) return fail(KVC_ERR_INVALID_ARG, "%s: n=%lld out of range", W, (long long)n);
   if (n_q_heads < 0 || n_k_heads < 0 || n_v_heads < 0 || n_q_heads + n_k_heads + n_v_heads < 1 ||
       n_q_heads + n_k_heads + n_v_heads > 1024)
@@ -869,7 +869,12 @@ kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k
       return fail(KVC_ERR_INVALID_ARG, "%s: rope_theta must be finite and > 0", W);
     for (int j = 0; j < kvc::kHalf; ++j) f[j] = std::pow(rope_theta, -(2.0 * j) / head_dim);
   }
+  if (norm && (!(norm->eps >= 0.0f) || !std::isfinite(norm->eps)))
+    return fail(KVC_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", W);
   if (n == 0) return ok();
+  if (norm && ((n_q_heads > 0 && (!norm->gamma_q || !aligned16(norm->gamma_q))) ||
+               (n_k_heads > 0 && (!norm->gamma_k || !aligned16(norm->gamma_k)))))
+    return fail(KVC_ERR_INVALID_ARG, "%s: gamma NULL or misaligned", W);
   if (!y || !aligned16(y) || (n_q_heads > 0 && (!q || !aligned16(q))) ||
       (n_k_heads > 0 && (!k || !aligned16(k))) || (n_v_heads > 0 && (!v || !aligned16(v))) ||
       (pos && (reinterpret_cast<uintptr_t>(pos) & 3u)))
@@ -878,16 +883,34 @@ kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k
   const size_t qb = (size_t)n * n_q_heads * head_dim * 2, kb = (size_t)n * n_k_heads * head_dim * 2,
                vb = (size_t)n * n_v_heads * head_dim * 2;
   kvc_status st = check_disjoint(W, {{q, qb, "q"}, {k, kb, "k"}, {v, vb, "v"}},
-                                 {{y, yb, "y"}, {pos, (size_t)n * 4, "pos"}});
+                                 {{y, yb, "y"}, {pos, (size_t)n * 4, "pos"},
+                                  {norm && n_q_heads > 0 ? norm->gamma_q : nullptr, (size_t)head_dim * 2, "gamma_q"},
+                                  {norm && n_k_heads > 0 ? norm->gamma_k : nullptr, (size_t)head_dim * 2, "gamma_k"}});
   if (st != KVC_OK) return st;
   st = need_device(W);
   if (st != KVC_OK) return st;
   const hipError_t e = kvc::launch_qkv_rope(static_cast<const uint16_t*>(y), n, n_q_heads, n_k_heads,
                                             n_v_heads, pos, f, static_cast<uint16_t*>(q),
                                             static_cast<uint16_t*>(k), static_cast<uint16_t*>(v),
-                                            as_stream(stream));
+                                            as_stream(stream), norm);
   if (e != hipSuccess) return hip_fail(W, e);
   return ok();
+}
+
+kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads, int32_t n_v_heads,
+                        int32_t head_dim, const int32_t* pos, double rope_theta, const double* inv_freq,
+                        void* q, void* k, void* v, void* stream) {
+  return qkv_rope_impl("kvc_qkv_rope", y, n, n_q_heads, n_k_heads, n_v_heads, head_dim, nullptr, pos, rope_theta,
+                       inv_freq, q, k, v, stream);
+}
+
+kvc_status kvc_qkv_norm_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads, int32_t n_v_heads,
+                             int32_t head_dim, const void* gamma_q, const void* gamma_k, float eps,
+                             const int32_t* pos, double rope_theta, const double* inv_freq, void* q, void* k, void* v,
+                             void* stream) {
+  const kvc::HeadNorm norm = {static_cast<const uint16_t*>(gamma_q), static_cast<const uint16_t*>(gamma_k), eps};
+  return qkv_rope_impl("kvc_qkv_norm_rope", y, n, n_q_heads, n_k_heads, n_v_heads, head_dim, &norm, pos, rope_theta,
+                       inv_freq, q, k, v, stream);
 }
 
 kvc_status kvc_swiglu(const void* gate_up, int64_t n, int64_t inter, void* out, void* stream) {
@@ -1060,6 +1083,176 @@ kvc_status kvc_stage_layers(const kvc_layout* L, const kvc_plan* plan, int32_t n
     }
   }
   return ok();
+}
+
+}  // extern "C"
+
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// A pool's tables, checked (null or misaligned pointers, sizes whose row
+// numbers or products leave int32); counts: whether the call uses ref.
+kvc_status check_pages(const char* W, const kvc_pages* P, bool counts, kvc::PageTables* t) {
+  if (!P) return fail(KVC_ERR_INVALID_ARG, "%s: pages is NULL", W);
+  if (P->n_pages < 1 || P->n_slots < 0 || P->max_pages < 0)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_pages=%d (>= 1), n_slots=%d, max_pages=%d (>= 0)", W, P->n_pages, P->n_slots,
+                P->max_pages);
+  if (P->page_rows < 8 || P->page_rows > 1024 || (P->page_rows & (P->page_rows - 1)) != 0)
+    return fail(KVC_ERR_UNSUPPORTED, "%s: page_rows=%d (a power of two in [8, 1024])", W, P->page_rows);
+  if ((int64_t)P->n_pages * P->page_rows > kMaxRows || (int64_t)P->max_pages * P->page_rows > kMaxRows)
+    return fail(KVC_ERR_INVALID_ARG, "%s: more than 2^31 - 128 rows in the pool or in a slot", W);
+  if (P->n_slots > KVC_PAGES_MAX_SLOTS)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_slots=%d (at most %d)", W, P->n_slots, KVC_PAGES_MAX_SLOTS);
+  if ((int64_t)P->n_slots * P->max_pages > (int64_t)INT32_MAX)
+    return fail(KVC_ERR_INVALID_ARG, "%s: a table of more than 2^31 - 1 entries", W);
+  if ((counts && (!P->ref || !aligned4(P->ref))) || (P->n_slots > 0 && (!P->len || !aligned4(P->len))) ||
+      (P->n_slots > 0 && P->max_pages > 0 && (!P->table || !aligned4(P->table))))
+    return fail(KVC_ERR_INVALID_ARG, "%s: ref, table or len NULL or misaligned", W);
+  t->n_pages = P->n_pages;
+  t->page_shift = __builtin_ctz((unsigned)P->page_rows);
+  t->n_slots = P->n_slots;
+  t->max_pages = P->max_pages;
+  t->ref = P->ref;
+  t->table = P->table;
+  t->len = P->len;
+  return KVC_OK;
+}
+
+Span ref_span(const kvc_pages* P) { return {P->ref, (size_t)P->n_pages * 4, "ref"}; }
+Span table_span(const kvc_pages* P) { return {P->table, (size_t)P->n_slots * P->max_pages * 4, "table"}; }
+Span len_span(const kvc_pages* P) { return {P->len, (size_t)P->n_slots * 4, "len"}; }
+
+size_t pages_ws(const kvc_pages* P) { return kvc::pages_ws_bytes(P->n_pages, P->n_slots, P->max_pages); }
+
+kvc_status check_pages_ws(const char* W, const kvc_pages* P, const void* ws, size_t ws_bytes) {
+  if (!ws || !aligned16(ws)) return fail(KVC_ERR_INVALID_ARG, "%s: ws NULL or not 16-byte aligned", W);
+  if (ws_bytes < pages_ws(P)) return fail(KVC_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", W, ws_bytes, pages_ws(P));
+  return KVC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+kvc_status kvc_pages_workspace(const kvc_pages* P, size_t* bytes) {
+  const char* W = "kvc_pages_workspace";
+  kvc::PageTables t;
+  const kvc_status st = check_pages(W, P, true, &t);
+  if (st != KVC_OK) return st;
+  if (!bytes) return fail(KVC_ERR_INVALID_ARG, "%s: bytes is NULL", W);
+  *bytes = pages_ws(P);
+  return ok();
+}
+
+kvc_status kvc_pages_trim(const kvc_pages* P, const int32_t* keep, void* stream) {
+  const char* W = "kvc_pages_trim";
+  kvc::PageTables t;
+  kvc_status st = check_pages(W, P, true, &t);
+  if (st != KVC_OK) return st;
+  if (P->n_slots == 0) return ok();
+  if (!keep || !aligned4(keep)) return fail(KVC_ERR_INVALID_ARG, "%s: keep NULL or misaligned", W);
+  st = check_disjoint(W, {ref_span(P), table_span(P), len_span(P)}, {{keep, (size_t)P->n_slots * 4, "keep"}});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const hipError_t e = kvc::launch_pages_trim(t, keep, as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+kvc_status kvc_pages_fork(const kvc_pages* P, const int32_t* src_of, void* ws, size_t ws_bytes, void* stream) {
+  const char* W = "kvc_pages_fork";
+  kvc::PageTables t;
+  kvc_status st = check_pages(W, P, true, &t);
+  if (st != KVC_OK) return st;
+  if (P->n_slots == 0) return ok();
+  if (!src_of || !aligned4(src_of)) return fail(KVC_ERR_INVALID_ARG, "%s: src_of NULL or misaligned", W);
+  st = check_pages_ws(W, P, ws, ws_bytes);
+  if (st != KVC_OK) return st;
+  st = check_disjoint(W, {ref_span(P), table_span(P), len_span(P), {ws, ws_bytes, "ws"}},
+                      {{src_of, (size_t)P->n_slots * 4, "src_of"}});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const hipError_t e = kvc::launch_pages_fork(t, src_of, static_cast<int32_t*>(ws), as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+kvc_status kvc_pages_reserve(const kvc_pages* P, const int32_t* n_new, int32_t max_new, int32_t* rows,
+                             int32_t* copy_src, int32_t* copy_dst, int32_t* shortage, void* ws, size_t ws_bytes,
+                             void* stream) {
+  const char* W = "kvc_pages_reserve";
+  kvc::PageTables t;
+  kvc_status st = check_pages(W, P, true, &t);
+  if (st != KVC_OK) return st;
+  if (max_new < 1 || (int64_t)max_new * std::max(P->n_slots, 1) > kMaxRows)
+    return fail(KVC_ERR_INVALID_ARG, "%s: max_new=%d must be >= 1, and max_new x n_slots at most 2^31 - 128", W, max_new);
+  if (!shortage || !aligned4(shortage)) return fail(KVC_ERR_INVALID_ARG, "%s: shortage NULL or misaligned", W);
+  const size_t sb = (size_t)P->n_slots * 4;
+  if (P->n_slots > 0 && (!n_new || !rows || !copy_src || !copy_dst || !aligned4(n_new) || !aligned4(rows) ||
+                         !aligned4(copy_src) || !aligned4(copy_dst)))
+    return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
+  st = check_pages_ws(W, P, ws, ws_bytes);
+  if (st != KVC_OK) return st;
+  st = check_disjoint(W,
+                      {ref_span(P), table_span(P), len_span(P), {rows, sb * max_new, "rows"}, {copy_src, sb, "copy_src"},
+                       {copy_dst, sb, "copy_dst"}, {shortage, 8, "shortage"}, {ws, ws_bytes, "ws"}},
+                      {{n_new, sb, "n_new"}});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const hipError_t e = kvc::launch_pages_reserve(t, n_new, max_new, rows, copy_src, copy_dst, shortage,
+                                                 static_cast<int32_t*>(ws), as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+kvc_status kvc_pages_compact(const kvc_pages* P, int32_t* move_src, int32_t* move_dst, int32_t* counts, void* ws,
+                             size_t ws_bytes, void* stream) {
+  const char* W = "kvc_pages_compact";
+  kvc::PageTables t;
+  kvc_status st = check_pages(W, P, true, &t);
+  if (st != KVC_OK) return st;
+  const size_t mb = (size_t)(P->n_pages / 2) * 4;
+  if (!counts || !aligned4(counts) || (mb > 0 && (!move_src || !move_dst || !aligned4(move_src) || !aligned4(move_dst))))
+    return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
+  st = check_pages_ws(W, P, ws, ws_bytes);
+  if (st != KVC_OK) return st;
+  st = check_disjoint(W,
+                      {ref_span(P), table_span(P), len_span(P), {move_src, mb, "move_src"}, {move_dst, mb, "move_dst"},
+                       {counts, 8, "counts"}, {ws, ws_bytes, "ws"}},
+                      {});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const hipError_t e =
+      kvc::launch_pages_compact(t, move_src, move_dst, counts, static_cast<int32_t*>(ws), as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t* dst, int64_t n_pairs,
+                          const int32_t* count, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, void* k_pages,
+                          void* v_pages, void* stream) {
+  const char* W = "kvc_pages_copy";
+  kvc::PageTables t;
+  kvc_status st = check_pages(W, P, false, &t);
+  if (st != KVC_OK) return st;
+  st = check_heads(W, n_kv_heads, n_kv_heads, head_dim);
+  if (st != KVC_OK) return st;
+  if (n_pairs < 0 || n_pairs > kMaxRows || n_layers < 0 || n_layers > 65536)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_pairs=%lld or n_layers=%d out of range", W, (long long)n_pairs, n_layers);
+  if (n_pairs == 0 || n_layers == 0) return ok();
+  if (!src || !dst || !k_pages || !v_pages || !aligned4(src) || !aligned4(dst) || !aligned16(k_pages) ||
+      !aligned16(v_pages) || !aligned4(count))
+    return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
+  const size_t page = (size_t)P->page_rows * n_kv_heads * head_dim * 2, pool = page * P->n_pages * n_layers;
+  st = check_disjoint(W, {{k_pages, pool, "k_pages"}, {v_pages, pool, "v_pages"}},
+                      {{src, (size_t)n_pairs * 4, "src"}, {dst, (size_t)n_pairs * 4, "dst"}, {count, 4, "count"}});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const hipError_t e = kvc::launch_pages_copy(P->n_pages, (int64_t)page, n_layers, static_cast<uint16_t*>(k_pages),
+                                              static_cast<uint16_t*>(v_pages), src, dst, n_pairs, count, as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
 }
 
 }  // extern "C"

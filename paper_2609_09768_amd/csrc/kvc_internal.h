@@ -126,9 +126,15 @@ int64_t attention_work_items(int64_t n_sel, int n_q_heads, int n_kv_heads);
 hipError_t launch_rms_norm(const uint16_t* x, int64_t n_x_rows, const int32_t* rows, int64_t n,
                            int hidden, const uint16_t* gamma, float eps, uint16_t* out,
                            uint16_t* res_out, hipStream_t s);
+// norm: the RMS norms of the query and key heads before the rotation, or NULL.
+struct HeadNorm {
+  const uint16_t* gamma_q;
+  const uint16_t* gamma_k;
+  float eps;
+};
 hipError_t launch_qkv_rope(const uint16_t* y, int64_t n, int n_q, int n_k, int n_v,
                            const int32_t* pos, const double* freqs, uint16_t* q, uint16_t* k,
-                           uint16_t* v, hipStream_t s);
+                           uint16_t* v, hipStream_t s, const HeadNorm* norm = nullptr);
 hipError_t launch_swiglu(const uint16_t* gu, int64_t n, int64_t inter, uint16_t* out,
                          hipStream_t s);
 size_t attention_ws_bytes(int64_t n_sel, int n_q_heads, int n_kv_heads);
@@ -156,6 +162,74 @@ struct CopyList {
 bool copy_list_add(CopyList* L, void* dst, const void* src, size_t bytes);
 // host: the sources are in host memory.
 hipError_t launch_copy_list(const CopyList& L, bool host, hipStream_t s);
+
+// ---- pages of a cache pool (pages.hip) ------------------------------------------
+// The tables of a kvc_pages, checked: page_rows is 2^page_shift.
+struct PageTables {
+  int32_t n_pages, page_shift, n_slots, max_pages;
+  int32_t* ref;
+  int32_t* table;
+  int32_t* len;
+};
+// Scratch of fork, reserve and compact: a copy of the tables and lengths, or
+// an entry and a count per page and slot.
+inline size_t pages_ws_bytes(int64_t n_pages, int64_t n_slots, int64_t max_pages) {
+  const size_t fork = size_t(n_slots) * size_t(max_pages + 1), lists = 2 * size_t(n_pages) + 2 * size_t(n_slots);
+  return align256(4 * (fork > lists ? fork : lists) + 4);
+}
+hipError_t launch_pages_trim(const PageTables& P, const int32_t* keep, hipStream_t s);
+hipError_t launch_pages_fork(const PageTables& P, const int32_t* src_of, int32_t* ws, hipStream_t s);
+hipError_t launch_pages_reserve(const PageTables& P, const int32_t* n_new, int32_t max_new, int32_t* rows,
+                                int32_t* copy_src, int32_t* copy_dst, int32_t* shortage, int32_t* ws, hipStream_t s);
+hipError_t launch_pages_compact(const PageTables& P, int32_t* move_src, int32_t* move_dst, int32_t* counts,
+                                int32_t* ws, hipStream_t s);
+// page_bytes: a multiple of 2 KB; count: device, or NULL (all n_pairs).
+hipError_t launch_pages_copy(int32_t n_pages, int64_t page_bytes, int n_layers, uint16_t* k, uint16_t* v,
+                             const int32_t* src, const int32_t* dst, int64_t n_pairs, const int32_t* count,
+                             hipStream_t s);
+
+// ---- attention over a shared prefix and own pages (prefix_attention.hip) ----------
+size_t prefix_attention_ws_bytes(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
+                                 int page_rows, int max_pages);
+// Workgroups of its largest launch.
+int64_t prefix_attention_workgroups(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
+                                    int page_rows, int max_pages);
+hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t* kp, const uint16_t* vp,
+                                   int64_t n_prefix, const PageTables& pages, const uint16_t* kt, const uint16_t* vt,
+                                   int n_q_heads, int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws,
+                                   hipStream_t s);
+
+// ---- packed sequences (attention.hip) -----------------------------------------------
+// Work of one workgroup and kv head: eight units (32 queries of one head each)
+// of one sequence over key tiles tile0 .. tile0 + n_tiles - 1.  part: where
+// its partial results go, -1 if it has all of the keys.
+struct PackItem {
+  int32_t row0, len;     // the sequence's first row and its rows
+  int32_t block;         // its units are 8 block .. 8 block + 7
+  int32_t tile0, n_tiles;
+  int32_t part;
+  int32_t pad[2];
+};
+// A block whose keys were cut: parts first .. first + n_parts - 1.
+struct PackJoin {
+  int32_t row0, len, block, first, n_parts;
+  int32_t pad[3];
+};
+struct PackHeader {
+  uint64_t id;
+  int32_t n_items, n_joins, n_parts, pad;
+};
+inline size_t pack_items_offset() { return align256(sizeof(PackHeader)); }
+inline size_t pack_joins_offset(int64_t n_items) {
+  return pack_items_offset() + align256(sizeof(PackItem) * size_t(n_items));
+}
+// Partials of a part: 8 units of 32 queries, D sums and a log-sum each.
+inline size_t pack_ws_bytes(int64_t n_parts, int n_kv_heads) {
+  return align256(size_t(n_parts) * size_t(n_kv_heads) * 8 * 32 * (kHeadDim + 1) * sizeof(float));
+}
+hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_joins, int n_parts,
+                                   const uint16_t* q, const uint16_t* k, const uint16_t* v, int n_q_heads,
+                                   int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws, hipStream_t s);
 
 // ---- static scratch (static_scratch.hip) -------------------------------------
 // Size of the per-GPU device array behind kvc_blend_prefill_layer_noalloc

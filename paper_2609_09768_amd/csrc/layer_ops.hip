@@ -5,7 +5,8 @@
 // (Section 3.4; Section 4 setup), so these steps run on the selected rows:
 //   * RMS normalisation, optionally gathering the rows it normalises;
 //   * the split of the fused Q/K/V projection output into Q, K and V with
-//     RoPE applied to Q and K at each token's position;
+//     RoPE applied to Q and K at each token's position, and for models that
+//     normalise each query and key head, that norm in the same pass;
 //   * the gated SiLU of the feed-forward block.
 // The projections between them are in gemm.hip.
 //
@@ -116,6 +117,10 @@ struct QkvRopeArgs {
   uint16_t* q;
   uint16_t* k;
   uint16_t* v;
+  // of the form that normalises the heads
+  const uint16_t* gamma_q;
+  const uint16_t* gamma_k;
+  float eps;
   double f[kHalf];
 };
 
@@ -136,6 +141,44 @@ __device__ __forceinline__ void rotate8_f32(const uint4& a, const uint4& b, cons
   ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
 }
 
+// The RMS norm of a head of 128 in the registers of the eight lanes that hold
+// it (a: elements 8 jg .., b: 64 + 8 jg ..), in float32, then the rotation of
+// the unrounded values: x' = x / sqrt(mean x^2 + eps) * gamma, rounded once
+// after the rotation.  g: the head's 128 weights.
+__device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, const uint16_t* g, int jg, float eps,
+                                             const float* c, const float* s, uint4& oa, uint4& ob) {
+  const uint4 ga = *reinterpret_cast<const uint4*>(g + 8 * jg);
+  const uint4 gb = *reinterpret_cast<const uint4*>(g + kHalf + 8 * jg);
+  float ss = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = bf16x8_elem(a, e), y = bf16x8_elem(b, e);
+    ss = fmaf(x, x, ss);
+    ss = fmaf(y, y, ss);
+  }
+#pragma unroll
+  for (int m = 1; m <= 4; m <<= 1) ss += __shfl_xor(ss, m, 64);
+  const float inv = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + eps);
+  uint32_t ra[4], rb[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float lo[2], hi[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = 2 * e + i;
+      const float x = bf16x8_elem(a, j) * inv * bf16x8_elem(ga, j);
+      const float y = bf16x8_elem(b, j) * inv * bf16x8_elem(gb, j);
+      lo[i] = fmaf(x, c[j], -(y * s[j]));
+      hi[i] = fmaf(y, c[j], x * s[j]);
+    }
+    ra[e] = pack2(lo[0], lo[1]);
+    rb[e] = pack2(hi[0], hi[1]);
+  }
+  oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+  ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+}
+
+template <bool NORM>
 __global__ __launch_bounds__(64 * kRopeWaves) void qkv_rope_kernel(const QkvRopeArgs A) {
   const int lane = threadIdx.x & 63;
   // one row per wave at a time; the row index is the same in every lane, so
@@ -187,11 +230,13 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qkv_rope_kernel(const QkvRope
 #pragma unroll
     for (int t = 0; t < kRopeBatch; ++t) {
       const int h = h0 + 8 * t;
+      // the eight lanes that share a head take this branch together
       if (h < n_rot) {
         uint16_t* dst = h < A.n_q ? A.q + (i * A.n_q + h) * kHeadDim
                                   : A.k + (i * A.n_k + (h - A.n_q)) * kHeadDim;
         uint4 oa, ob;
-        rotate8_f32(a[t], b[t], c, s, oa, ob);
+        if constexpr (NORM) norm_rotate8(a[t], b[t], h < A.n_q ? A.gamma_q : A.gamma_k, jg, A.eps, c, s, oa, ob);
+        else rotate8_f32(a[t], b[t], c, s, oa, ob);
         *reinterpret_cast<uint4*>(dst + 8 * jg) = oa;
         *reinterpret_cast<uint4*>(dst + kHalf + 8 * jg) = ob;
       }
@@ -252,7 +297,7 @@ hipError_t launch_rms_norm(const uint16_t* x, int64_t n_x_rows, const int32_t* r
 
 hipError_t launch_qkv_rope(const uint16_t* y, int64_t n, int n_q, int n_k, int n_v,
                            const int32_t* pos, const double* freqs, uint16_t* q, uint16_t* k,
-                           uint16_t* v, hipStream_t s) {
+                           uint16_t* v, hipStream_t s, const HeadNorm* norm) {
   if (n <= 0) return hipSuccess;
   QkvRopeArgs A;
   A.y = y;
@@ -264,9 +309,13 @@ hipError_t launch_qkv_rope(const uint16_t* y, int64_t n, int n_q, int n_k, int n
   A.q = q;
   A.k = k;
   A.v = v;
+  A.gamma_q = norm ? norm->gamma_q : nullptr;
+  A.gamma_k = norm ? norm->gamma_k : nullptr;
+  A.eps = norm ? norm->eps : 0.0f;
   for (int j = 0; j < kHalf; ++j) A.f[j] = freqs[j];
-  hipLaunchKernelGGL(qkv_rope_kernel, dim3((unsigned)std::min<int64_t>((n + kRopeWaves - 1) / kRopeWaves, kMaxGrid)),
-                     dim3(64 * kRopeWaves), 0, s, A);
+  const dim3 grid((unsigned)std::min<int64_t>((n + kRopeWaves - 1) / kRopeWaves, kMaxGrid)), block(64 * kRopeWaves);
+  if (norm) hipLaunchKernelGGL(qkv_rope_kernel<true>, grid, block, 0, s, A);
+  else hipLaunchKernelGGL(qkv_rope_kernel<false>, grid, block, 0, s, A);
   return hipGetLastError();
 }
 
