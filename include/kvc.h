@@ -461,6 +461,50 @@ kvc_status kvc_stage_layers(const kvc_layout* L, const kvc_plan* plan, int32_t n
                             void* stream);
 
 /*
+ * Packed sequences: where a request's chunk caches come from.  Each chunk is
+ * prefilled on its own, many of them back to back in one batch: sequence s has
+ * seq_len[s] rows, the rows behind those of sequence s - 1.
+ */
+typedef struct kvc_pack {
+  int32_t n_seqs;          /* >= 0 */
+  const int32_t* seq_len;  /* host [n_seqs], each >= 0; NULL only if n_seqs == 0 */
+  int32_t n_q_heads;       /* Hq >= 1, multiple of n_kv_heads */
+  int32_t n_kv_heads;      /* Hkv >= 1 */
+  int32_t head_dim;        /* D, must be 128 */
+} kvc_pack;
+
+/*
+ * The plan of a packed batch: its work items, longest first, for every layer of
+ * the batch.  Built, copied and described as by kvc_plan_upload (host_staging
+ * NULL: the call waits for its copy); the descriptor's layout_id identifies
+ * lengths and heads, and kvc_packed_attention refuses a plan of other ones.
+ */
+kvc_status kvc_pack_plan_bytes(const kvc_pack* P, size_t* bytes);
+kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_bytes, void* host_staging,
+                                kvc_plan* plan_out, void* stream);
+
+/*
+ * Causal GQA attention inside each packed sequence.  For row i of a sequence
+ * that starts at row b, query head h, kv head g = h / (Hq / Hkv):
+ *   s_j = scale * <q[b+i,h], k[b+j,g]> for j = 0..i,
+ *   out[b+i,h] = sum_j softmax(s)_j v[b+j,g],  lse[b+i,h] = ln sum_j exp(s_j).
+ * q, out: device bf16 [n_rows, Hq, D]; k, v: device bf16 [n_rows, Hkv, D]; lse:
+ * device float32 [n_rows, Hq] or NULL; n_rows at least the sum of the lengths.
+ * Rows behind the last sequence are neither read nor written, and no sequence
+ * sees what another's rows hold.  softmax_scale 0 means 1/sqrt(D).  bf16 MFMA,
+ * float32 scores, softmax and sums; the weights are rounded to bf16 for the
+ * product with V.  ws: kvc_packed_attention_workspace bytes (0 for most
+ * batches: few long sequences get their keys cut over several workgroups),
+ * 16-byte aligned, KVC_ERR_WORKSPACE below that.  The same call gives the same
+ * bits.  Blocks x kv heads of one launch are at most 2^22, a block being eight
+ * (32 queries, head) units of a kv head (KVC_ERR_INVALID_ARG above).
+ */
+kvc_status kvc_packed_attention_workspace(const kvc_pack* P, size_t* bytes);
+kvc_status kvc_packed_attention(const kvc_pack* P, const kvc_plan* plan, const void* q, const void* k,
+                                const void* v, int64_t n_rows, float softmax_scale, void* out, float* lse,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Pages: the rows that sequences add behind a shared context (generated
  * tokens, a question of their own), in pages of a pool, so that sequences
  * grow, end, continue each other and share rows without their rows moving.
@@ -553,6 +597,40 @@ kvc_status kvc_pages_compact(const kvc_pages* P, int32_t* move_src, int32_t* mov
 kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t* dst, int64_t n_pairs,
                           const int32_t* count, int32_t n_layers, int32_t n_kv_heads, int32_t head_dim,
                           void* k_pages, void* v_pages, void* stream);
+
+/*
+ * Attention of a batch over one shared prefix and over pages of its own: the
+ * tokens that sequences add behind the blended context.  The sequences are the
+ * slots of P, whose last n_new rows are the query tokens (their keys and values
+ * already written); every one of them sees the whole prefix, whose rows are
+ * read once for all of them.  For query i of slot s, t = len[s] - n_new + i:
+ *   out[s,i,h] = sum softmax over prefix rows 0 .. n_prefix - 1 and the slot's
+ *   own rows 0 .. t together, with kv head h / (Hq / Hkv); lse[s,i,h] the
+ *   logarithm of the sum of exponentials.
+ * A query with t < 0 (a slot that is not in use, or a shorter one in a batch
+ * padded on the left) gets out = 0 and lse = -inf.
+ * q, out: device bf16 [n_slots, n_new, Hq, D]; lse: device float32 [n_slots,
+ * n_new, Hq] or NULL; n_new in [1, KVC_SHARED_MAX_NEW] (1: decoding).
+ * k_prefix, v_prefix: device bf16 [n_prefix, Hkv, D], e.g. a layer's blended
+ * cache (NULL only if n_prefix == 0); k_pages, v_pages: device bf16 [n_pages,
+ * page_rows, Hkv, D], one layer's pool.  Rows of a page behind a slot's length
+ * may hold anything, NaN among it; rows of a table entry outside [0, n_pages)
+ * are left out.  P->ref is not used.  softmax_scale 0 means 1/sqrt(D).  bf16
+ * MFMA, float32 scores, softmax and sums; the weights are rounded to bf16 for
+ * the product with V.  ws: kvc_shared_prefix_workspace bytes (a part's float32
+ * results for each part of the keys, so it grows with max_pages), 16-byte
+ * aligned.  The same call gives the same bits.  n_slots x n_new x Hq is at
+ * most 2^25.
+ */
+#define KVC_SHARED_MAX_NEW 4096
+kvc_status kvc_shared_prefix_workspace(const kvc_pages* P, int64_t n_prefix, int32_t n_new,
+                                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                       size_t* bytes);
+kvc_status kvc_shared_prefix_attention(const void* q, int32_t n_new, const void* k_prefix,
+                                       const void* v_prefix, int64_t n_prefix, const kvc_pages* P,
+                                       const void* k_pages, const void* v_pages, int32_t n_q_heads,
+                                       int32_t n_kv_heads, int32_t head_dim, float softmax_scale, void* out,
+                                       float* lse, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -52,12 +52,18 @@ class kvc_plan(ctypes.Structure):
     _fields_ = [("device", _vp), ("bytes", _sz), ("layout_id", ctypes.c_uint64)]
 
 
+class kvc_pack(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("seq_len", ctypes.POINTER(_i32)), ("n_q_heads", _i32), ("n_kv_heads", _i32),
+                ("head_dim", _i32)]
+
+
 class kvc_pages(ctypes.Structure):
     _fields_ = [("n_pages", _i32), ("page_rows", _i32), ("n_slots", _i32), ("max_pages", _i32),
                 ("ref", _vp), ("table", _vp), ("len", _vp)]
 
 
 _LP = ctypes.POINTER(kvc_layout)
+_PKP = ctypes.POINTER(kvc_pack)
 _PGP = ctypes.POINTER(kvc_pages)
 _PLP = ctypes.POINTER(kvc_plan)
 _PP = ctypes.POINTER(_vp)
@@ -91,6 +97,13 @@ _SIGS = {
     "kvc_projection": (_i32, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp]),
     "kvc_stage_layer": (_i32, [_LP, _PLP, _PP, _PP, _vp, _vp, _vp]),
     "kvc_stage_layers": (_i32, [_LP, _PLP, _i32, _PP, _PP, _PP, _PP, _PP, _vp]),
+    "kvc_pack_plan_bytes": (_i32, [_PKP, ctypes.POINTER(_sz)]),
+    "kvc_pack_plan_upload": (_i32, [_PKP, _vp, _sz, _vp, _PLP, _vp]),
+    "kvc_packed_attention_workspace": (_i32, [_PKP, ctypes.POINTER(_sz)]),
+    "kvc_packed_attention": (_i32, [_PKP, _PLP, _vp, _vp, _vp, _i64, _f32, _vp, _vp, _vp, _sz, _vp]),
+    "kvc_shared_prefix_workspace": (_i32, [_PGP, _i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "kvc_shared_prefix_attention": (_i32, [_vp, _i32, _vp, _vp, _i64, _PGP, _vp, _vp, _i32, _i32, _i32, _f32, _vp, _vp,
+                                           _vp, _sz, _vp]),
     "kvc_pages_workspace": (_i32, [_PGP, ctypes.POINTER(_sz)]),
     "kvc_pages_trim": (_i32, [_PGP, _vp, _vp]),
     "kvc_pages_fork": (_i32, [_PGP, _vp, _vp, _sz, _vp]),
@@ -359,6 +372,51 @@ def kvc_stage_layers(layout, plan, n_layers, k_chunks, v_chunks, k_cache, v_cach
                                  _ptrs(k_cache), _ptrs(v_cache), _ptrs(ev), _stream(stream)))
 
 
+class Pack:
+    """Owns the host array behind a ``kvc_pack`` (see include/kvc.h)."""
+
+    def __init__(self, seq_len, n_q_heads, n_kv_heads, head_dim=128):
+        self.seq_len = [int(x) for x in seq_len]
+        self._len = (_i32 * max(len(self.seq_len), 1))(*self.seq_len)
+        self.struct = kvc_pack(len(self.seq_len), ctypes.cast(self._len, ctypes.POINTER(_i32)), int(n_q_heads),
+                               int(n_kv_heads), int(head_dim))
+
+    @property
+    def n_rows(self) -> int:
+        return sum(self.seq_len)
+
+    def ref(self):
+        return ctypes.byref(self.struct)
+
+
+def kvc_pack_plan_bytes(pack) -> int:
+    b = _sz(0)
+    _check(_lib.kvc_pack_plan_bytes(_lref(pack), ctypes.byref(b)))
+    return b.value
+
+
+def kvc_pack_plan_upload(pack, plan, plan_bytes, stream=None, staging=None) -> Plan:
+    """As kvc_plan_upload, for a packed batch."""
+    out = kvc_plan()
+    _check(_lib.kvc_pack_plan_upload(_lref(pack), _ptr(plan), int(plan_bytes), _ptr(staging), ctypes.byref(out),
+                                     _stream(stream)))
+    p = Plan(plan, out.bytes, out.layout_id, keep=() if staging is None else (staging,))
+    p.struct.device = out.device
+    return p
+
+
+def kvc_packed_attention_workspace(pack) -> int:
+    b = _sz(0)
+    _check(_lib.kvc_packed_attention_workspace(_lref(pack), ctypes.byref(b)))
+    return b.value
+
+
+def kvc_packed_attention(pack, plan, q, k, v, n_rows, softmax_scale, out, lse, ws=None, ws_bytes=0, stream=None):
+    _check(_lib.kvc_packed_attention(_lref(pack), _pref(plan), _ptr(q), _ptr(k), _ptr(v), int(n_rows),
+                                     float(softmax_scale), _ptr(out), _ptr(lse), _ptr(ws), int(ws_bytes),
+                                     _stream(stream)))
+
+
 class Pages:
     """A ``kvc_pages`` (see include/kvc.h) plus references to its device arrays."""
 
@@ -406,4 +464,20 @@ def kvc_pages_copy(pages, src, dst, n_pairs, count, n_layers, n_kv_heads, head_d
                                int(n_kv_heads), int(head_dim), _ptr(k_pages), _ptr(v_pages), _stream(stream)))
 
 
-__all__ = [n for n in _SIGS] + ["Layout", "Plan", "KvcError", "LIB_PATH", "kvc_layout", "kvc_plan", "Pages", "kvc_pages"]
+def kvc_shared_prefix_workspace(pages, n_prefix, n_new, n_q_heads, n_kv_heads, head_dim) -> int:
+    b = _sz(0)
+    _check(_lib.kvc_shared_prefix_workspace(_pgref(pages), int(n_prefix), int(n_new), int(n_q_heads),
+                                            int(n_kv_heads), int(head_dim), ctypes.byref(b)))
+    return b.value
+
+
+def kvc_shared_prefix_attention(q, n_new, k_prefix, v_prefix, n_prefix, pages, k_pages, v_pages, n_q_heads,
+                                n_kv_heads, head_dim, softmax_scale, out, lse, ws, ws_bytes, stream=None):
+    _check(_lib.kvc_shared_prefix_attention(
+        _ptr(q), int(n_new), _ptr(k_prefix), _ptr(v_prefix), int(n_prefix), _pgref(pages), _ptr(k_pages),
+        _ptr(v_pages), int(n_q_heads), int(n_kv_heads), int(head_dim), float(softmax_scale), _ptr(out), _ptr(lse),
+        _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+__all__ = [n for n in _SIGS] + ["Layout", "Plan", "KvcError", "LIB_PATH", "kvc_layout", "kvc_plan", "Pack", "Pages", "kvc_pack",
+                                "kvc_pages"]

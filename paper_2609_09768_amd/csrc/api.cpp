@@ -1256,3 +1256,281 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
 }
 
 }  // extern "C"
+
+namespace {
+
+// ---- packed sequences -------------------------------------------------------------
+constexpr int kPackUnits = 8;   // units of 32 queries and a head in a workgroup
+constexpr int kPackTile = 64;   // keys of a tile
+constexpr int kCus = 256;
+
+// A block of a sequence: units 8 block .. 8 block + 7 of ceil(len / 32) groups
+// of queries times `group` heads, and the key tiles up to its last query.
+int64_t pack_blocks(int64_t len, int group) { return ((len + 31) / 32 * group + kPackUnits - 1) / kPackUnits; }
+int pack_tiles(int64_t len, int group, int64_t block) {
+  const int64_t last = std::min<int64_t>(32 * ((kPackUnits * block + kPackUnits - 1) / group + 1), len) - 1;
+  return (int)(last / kPackTile) + 1;
+}
+// Parts a block's tiles are cut into.  Blocks run longest first, so the batch
+// takes about the larger of a CU's share of all tiles and the longest block:
+// one that is a quarter longer than the share is cut into parts of about the
+// share, but of no less than kPackLeast tiles, since a workgroup costs about as
+// much as that before and after its tiles.
+constexpr int kPackLeast = 8;
+int pack_parts(int tiles, int64_t share) {
+  const int64_t part = std::max<int64_t>(share, kPackLeast);
+  return 4 * (int64_t)tiles > 5 * part ? (int)((tiles + part - 1) / part) : 1;
+}
+
+struct PackInfo {
+  int64_t n_rows = 0, n_items = 0, n_joins = 0, n_parts = 0;
+  int64_t share = 0;  // about a CU's share of the key tiles
+};
+
+kvc_status check_pack(const char* W, const kvc_pack* P, PackInfo* info) {
+  if (!P) return fail(KVC_ERR_INVALID_ARG, "%s: pack is NULL", W);
+  if (P->n_seqs < 0) return fail(KVC_ERR_INVALID_ARG, "%s: n_seqs=%d < 0", W, P->n_seqs);
+  if (P->n_seqs > 0 && !P->seq_len) return fail(KVC_ERR_INVALID_ARG, "%s: seq_len is NULL", W);
+  kvc_status st = check_heads(W, P->n_q_heads, P->n_kv_heads, P->head_dim);
+  if (st != KVC_OK) return st;
+  const int group = P->n_q_heads / P->n_kv_heads;
+  PackInfo i;
+  int64_t twice = 0;  // tiles of all blocks, twice: blocks x (first + last block's tiles)
+  int longest = 0;
+  for (int32_t s = 0; s < P->n_seqs; ++s) {
+    const int32_t len = P->seq_len[s];
+    if (len < 0) return fail(KVC_ERR_INVALID_ARG, "%s: seq_len[%d]=%d < 0", W, s, len);
+    if (len == 0) continue;
+    i.n_rows += len;
+    if (i.n_rows > kMaxRows) return fail(KVC_ERR_INVALID_ARG, "%s: too many rows", W);
+    const int64_t n = pack_blocks(len, group);
+    const int tiles = pack_tiles(len, group, n - 1);
+    i.n_items += n;
+    twice += n * (pack_tiles(len, group, 0) + tiles);
+    longest = std::max(longest, tiles);
+  }
+  // one launch: fewer than 2^32 work-items, cut blocks included (those are
+  // cut only where there are few, see pack_parts)
+  if (i.n_items * P->n_kv_heads > (int64_t(1) << 22))
+    return fail(KVC_ERR_INVALID_ARG, "%s: too many queries and heads for one launch", W);
+  i.share = (twice * P->n_kv_heads + 2 * kCus - 1) / (2 * kCus);
+  if (pack_parts(longest, i.share) > 1)
+    for (int32_t s = 0; s < P->n_seqs; ++s)
+      for (int64_t b = 0, n = pack_blocks(P->seq_len[s], group); b < n; ++b) {
+        const int parts = pack_parts(pack_tiles(P->seq_len[s], group, b), i.share);
+        if (parts == 1) continue;
+        i.n_items += parts - 1;
+        i.n_parts += parts;
+        ++i.n_joins;
+      }
+  if (info) *info = i;
+  return KVC_OK;
+}
+
+uint64_t pack_id(const kvc_pack* P) {
+  uint64_t h = fnv(1469598103934665603ull, "packed sequences", 16);
+  h = fnv(h, &P->n_q_heads, sizeof(P->n_q_heads));
+  h = fnv(h, &P->n_kv_heads, sizeof(P->n_kv_heads));
+  h = fnv(h, &P->head_dim, sizeof(P->head_dim));
+  h = fnv(h, &P->n_seqs, sizeof(P->n_seqs));
+  if (P->n_seqs > 0) h = fnv(h, P->seq_len, sizeof(int32_t) * (size_t)P->n_seqs);
+  return h | 1ull;
+}
+
+size_t pack_bytes(const PackInfo& i) {
+  return kvc::pack_joins_offset(i.n_items) + kvc::align256(sizeof(kvc::PackJoin) * (size_t)i.n_joins);
+}
+
+// The plan's image: work items, those with the most tiles first.
+void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
+  const int group = P->n_q_heads / P->n_kv_heads;
+  kvc::PackHeader hdr;
+  std::memset(&hdr, 0, sizeof(hdr));
+  hdr.id = pack_id(P);
+  hdr.n_items = (int32_t)info.n_items;
+  hdr.n_joins = (int32_t)info.n_joins;
+  hdr.n_parts = (int32_t)info.n_parts;
+  std::memcpy(img, &hdr, sizeof(hdr));
+  kvc::PackItem* items = reinterpret_cast<kvc::PackItem*>(img + kvc::pack_items_offset());
+  kvc::PackJoin* joins = reinterpret_cast<kvc::PackJoin*>(img + kvc::pack_joins_offset(info.n_items));
+  int64_t row0 = 0, n = 0, nj = 0, np = 0;
+  for (int32_t s = 0; s < P->n_seqs; ++s) {
+    const int32_t len = P->seq_len[s];
+    for (int64_t b = 0, nb = pack_blocks(len, group); b < nb; ++b) {
+      const int tiles = pack_tiles(len, group, b), parts = pack_parts(tiles, info.share);
+      if (parts > 1) joins[nj++] = {(int32_t)row0, len, (int32_t)b, (int32_t)np, parts, {0, 0, 0}};
+      for (int i = 0; i < parts; ++i) {
+        const int t0 = (int)((int64_t)tiles * i / parts), t1 = (int)((int64_t)tiles * (i + 1) / parts);
+        items[n++] = {(int32_t)row0, len, (int32_t)b, t0, t1 - t0, parts > 1 ? (int32_t)np++ : -1, {0, 0}};
+      }
+    }
+    row0 += len;
+  }
+  std::stable_sort(items, items + n, [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; });
+}
+
+}  // namespace
+
+extern "C" {
+
+kvc_status kvc_pack_plan_bytes(const kvc_pack* P, size_t* bytes) {
+  const char* W = "kvc_pack_plan_bytes";
+  PackInfo i;
+  const kvc_status st = check_pack(W, P, &i);
+  if (st != KVC_OK) return st;
+  if (!bytes) return fail(KVC_ERR_INVALID_ARG, "%s: bytes is NULL", W);
+  *bytes = pack_bytes(i);
+  return ok();
+}
+
+kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_bytes_in, void* host_staging,
+                                kvc_plan* plan_out, void* stream) {
+  const char* W = "kvc_pack_plan_upload";
+  PackInfo info;
+  kvc_status st = check_pack(W, P, &info);
+  if (st != KVC_OK) return st;
+  if (!plan_dev || !aligned16(plan_dev)) return fail(KVC_ERR_INVALID_ARG, "%s: plan is NULL or not 16-byte aligned", W);
+  if (!plan_out) return fail(KVC_ERR_INVALID_ARG, "%s: plan_out is NULL", W);
+  const size_t need = pack_bytes(info);
+  if (plan_bytes_in < need)
+    return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan_bytes_in, need);
+  std::vector<unsigned char> own;
+  unsigned char* img = static_cast<unsigned char*>(host_staging);
+  if (!img) {
+    own.assign(need, 0);
+    img = own.data();
+  } else {
+    std::memset(img, 0, need);
+  }
+  build_pack(P, info, img);
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  hipError_t e = hipMemcpyAsync(plan_dev, img, need, hipMemcpyHostToDevice, as_stream(stream));
+  if (e == hipSuccess && !host_staging) e = hipStreamSynchronize(as_stream(stream));
+  if (e != hipSuccess) return hip_fail(W, e);
+  plan_out->device = plan_dev;
+  plan_out->bytes = plan_bytes_in;
+  plan_out->layout_id = pack_id(P);
+  return ok();
+}
+
+kvc_status kvc_packed_attention_workspace(const kvc_pack* P, size_t* bytes) {
+  const char* W = "kvc_packed_attention_workspace";
+  PackInfo i;
+  const kvc_status st = check_pack(W, P, &i);
+  if (st != KVC_OK) return st;
+  if (!bytes) return fail(KVC_ERR_INVALID_ARG, "%s: bytes is NULL", W);
+  *bytes = i.n_parts > 0 ? kvc::pack_ws_bytes(i.n_parts, P->n_kv_heads) : 0;
+  return ok();
+}
+
+kvc_status kvc_packed_attention(const kvc_pack* P, const kvc_plan* plan, const void* q, const void* k, const void* v,
+                                int64_t n_rows, float softmax_scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                                void* stream) {
+  const char* W = "kvc_packed_attention";
+  PackInfo i;
+  kvc_status st = check_pack(W, P, &i);
+  if (st != KVC_OK) return st;
+  if (n_rows < i.n_rows || n_rows > kMaxRows)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_rows=%lld, the sequences have %lld", W, (long long)n_rows, (long long)i.n_rows);
+  if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale))
+    return fail(KVC_ERR_INVALID_ARG, "%s: softmax_scale must be finite and >= 0", W);
+  if (i.n_rows == 0) return ok();
+  if (!plan || !plan->device || !aligned16(plan->device))
+    return fail(KVC_ERR_INVALID_ARG, "%s: plan is NULL, or its buffer NULL or not 16-byte aligned", W);
+  const uint64_t id = pack_id(P);
+  if (plan->layout_id != id)
+    return fail(KVC_ERR_INVALID_ARG, "%s: the plan was built for other sequences (id %016llx, these %016llx)", W,
+                (unsigned long long)plan->layout_id, (unsigned long long)id);
+  if (plan->bytes < pack_bytes(i))
+    return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan->bytes, pack_bytes(i));
+  if (!q || !k || !v || !out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(lse))
+    return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
+  const size_t need = i.n_parts > 0 ? kvc::pack_ws_bytes(i.n_parts, P->n_kv_heads) : 0;
+  if (need > 0 && (!ws || !aligned16(ws))) return fail(KVC_ERR_INVALID_ARG, "%s: ws NULL or not 16-byte aligned", W);
+  if (ws_bytes < need) return fail(KVC_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", W, ws_bytes, need);
+  const size_t qr = (size_t)P->n_q_heads * P->head_dim * 2, kr = (size_t)P->n_kv_heads * P->head_dim * 2;
+  st = check_disjoint(W,
+                      {{out, (size_t)n_rows * qr, "out"}, {lse, (size_t)n_rows * P->n_q_heads * 4, "lse"},
+                       {ws, ws_bytes, "ws"}},
+                      {{q, (size_t)n_rows * qr, "q"}, {k, (size_t)n_rows * kr, "k"}, {v, (size_t)n_rows * kr, "v"},
+                       plan_span(plan)});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)P->head_dim);
+  const hipError_t e = kvc::launch_packed_attention(
+      plan->device, id, (int)i.n_items, (int)i.n_joins, (int)i.n_parts, static_cast<const uint16_t*>(q),
+      static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), P->n_q_heads, P->n_kv_heads, scale,
+      static_cast<uint16_t*>(out), lse, ws, as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+// Checks of the attention over a shared prefix that do not need its tensors.
+static kvc_status check_shared(const char* W, const kvc_pages* P, int64_t n_prefix, int32_t n_new, int32_t n_q_heads,
+                               int32_t n_kv_heads, int32_t head_dim, kvc::PageTables* t) {
+  kvc_status st = check_pages(W, P, false, t);
+  if (st != KVC_OK) return st;
+  st = check_heads(W, n_q_heads, n_kv_heads, head_dim);
+  if (st != KVC_OK) return st;
+  if (n_prefix < 0 || n_prefix > kMaxRows)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_prefix=%lld out of range", W, (long long)n_prefix);
+  if (n_new < 1 || n_new > KVC_SHARED_MAX_NEW)
+    return fail(KVC_ERR_INVALID_ARG, "%s: n_new=%d must be in [1, %d]", W, n_new, KVC_SHARED_MAX_NEW);
+  // one launch: fewer than 2^32 work-items, 64 for each query and head
+  if ((int64_t)P->n_slots * n_new * n_q_heads > (int64_t(1) << 25) ||
+      kvc::prefix_attention_workgroups(n_prefix, P->n_slots, n_new, n_q_heads, n_kv_heads, P->page_rows, P->max_pages) >
+          (int64_t(1) << 22))
+    return fail(KVC_ERR_INVALID_ARG, "%s: too many slots, queries and heads for one launch", W);
+  return KVC_OK;
+}
+
+kvc_status kvc_shared_prefix_workspace(const kvc_pages* P, int64_t n_prefix, int32_t n_new, int32_t n_q_heads,
+                                       int32_t n_kv_heads, int32_t head_dim, size_t* bytes) {
+  const char* W = "kvc_shared_prefix_workspace";
+  kvc::PageTables t;
+  const kvc_status st = check_shared(W, P, n_prefix, n_new, n_q_heads, n_kv_heads, head_dim, &t);
+  if (st != KVC_OK) return st;
+  if (!bytes) return fail(KVC_ERR_INVALID_ARG, "%s: bytes is NULL", W);
+  *bytes = kvc::prefix_attention_ws_bytes(n_prefix, P->n_slots, n_new, n_q_heads, n_kv_heads, P->page_rows, P->max_pages);
+  return ok();
+}
+
+kvc_status kvc_shared_prefix_attention(const void* q, int32_t n_new, const void* k_prefix, const void* v_prefix,
+                                       int64_t n_prefix, const kvc_pages* P, const void* k_pages, const void* v_pages,
+                                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale,
+                                       void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* W = "kvc_shared_prefix_attention";
+  kvc::PageTables t;
+  kvc_status st = check_shared(W, P, n_prefix, n_new, n_q_heads, n_kv_heads, head_dim, &t);
+  if (st != KVC_OK) return st;
+  if (!(softmax_scale >= 0.0f) || !std::isfinite(softmax_scale))
+    return fail(KVC_ERR_INVALID_ARG, "%s: softmax_scale must be finite and >= 0", W);
+  if (P->n_slots == 0) return ok();
+  if (!q || !out || !aligned16(q) || !aligned16(out) || !aligned4(lse) ||
+      (n_prefix > 0 && (!k_prefix || !v_prefix || !aligned16(k_prefix) || !aligned16(v_prefix))) ||
+      (P->max_pages > 0 && (!k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages))))
+    return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
+  const size_t need =
+      kvc::prefix_attention_ws_bytes(n_prefix, P->n_slots, n_new, n_q_heads, n_kv_heads, P->page_rows, P->max_pages);
+  if (need > 0 && (!ws || !aligned16(ws))) return fail(KVC_ERR_INVALID_ARG, "%s: ws NULL or not 16-byte aligned", W);
+  if (ws_bytes < need) return fail(KVC_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", W, ws_bytes, need);
+  const size_t queries = (size_t)P->n_slots * n_new, qb = queries * n_q_heads * head_dim * 2;
+  const size_t kr = (size_t)n_kv_heads * head_dim * 2, pool = (size_t)P->n_pages * P->page_rows * kr;
+  st = check_disjoint(W, {{out, qb, "out"}, {lse, queries * n_q_heads * 4, "lse"}, {ws, ws_bytes, "ws"}},
+                      {{q, qb, "q"}, {k_prefix, (size_t)n_prefix * kr, "k_prefix"},
+                       {v_prefix, (size_t)n_prefix * kr, "v_prefix"}, {P->max_pages > 0 ? k_pages : nullptr, pool, "k_pages"},
+                       {P->max_pages > 0 ? v_pages : nullptr, pool, "v_pages"}, table_span(P), len_span(P)});
+  if (st != KVC_OK) return st;
+  st = need_device(W);
+  if (st != KVC_OK) return st;
+  const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)head_dim);
+  const hipError_t e = kvc::launch_prefix_attention(
+      static_cast<const uint16_t*>(q), n_new, static_cast<const uint16_t*>(k_prefix),
+      static_cast<const uint16_t*>(v_prefix), n_prefix, t, static_cast<const uint16_t*>(k_pages),
+      static_cast<const uint16_t*>(v_pages), n_q_heads, n_kv_heads, scale, static_cast<uint16_t*>(out), lse, ws,
+      as_stream(stream));
+  return e != hipSuccess ? hip_fail(W, e) : ok();
+}
+
+}  // extern "C"

@@ -118,6 +118,11 @@ struct AttnParams {
   float* part_o;    // [n_split][kv head][n_sel x G pairs][D], see first_pair
   float* part_lse;  // [n_split][kv head][n_sel x G pairs]
   int units;        // units of a workgroup, at most its waves
+  // packed sequences: the plan's work items, and the id its header must hold
+  const PackHeader* plan;
+  const PackItem* items;
+  const PackJoin* joins;
+  unsigned long long plan_id;
 };
 
 // Query-head pairs of a kv head before unit u: 32 for a unit, fewer for the
@@ -142,7 +147,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
 
 // UNITS: units of a workgroup, 0 where only P.units says (which costs 0.4 us
 // before the first loads, of the 31 of a check layer of 1,024 rows).
-template <int UNITS>
+// PACKED: every query of many sequences that lie back to back, causal inside
+// each (chunks prefilled on their own).  Blocks, their order and their shares
+// of the key tiles come from the plan's work items; the rest is the same.
+// The weights' sums are taken before they are rounded to bf16, one more
+// addition per pair, which makes the log-sum exact to float32.
+template <int UNITS, bool PACKED = false>
 __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams P) {
   // one array per slot, so alias analysis can tell a slot being loaded
   // from the slots being read
@@ -160,21 +170,32 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 
   const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
   const unsigned rest = blockIdx.x / (unsigned)P.n_kv_heads;
-  const int split = (int)(rest % (unsigned)P.n_split);
-  const int block = P.n_blocks - 1 - (int)(rest / (unsigned)P.n_split);
-  const long long n_kv = P.n_kv;
+  PackItem item = {};
+  if constexpr (PACKED) {
+    item = P.items[rest];
+    if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
+  }
+  const int split = PACKED ? 0 : (int)(rest % (unsigned)P.n_split);
+  const int block = PACKED ? item.block : P.n_blocks - 1 - (int)(rest / (unsigned)P.n_split);
+  const long long n_kv = PACKED ? item.len : P.n_kv;
+  const long long n_sel = PACKED ? item.len : P.n_sel;
+  const int n_subs = PACKED ? (item.len + 31) / 32 : P.n_subs;
+  const long long row0 = PACKED ? item.row0 : 0;
 
   // this wave's unit and this lane's query (one per lane pair l, l^32); a wave
   // past the workgroup's units has none, like the units past the last group
   const int units = UNITS ? UNITS : P.units;
   const int unit = units * block + wave;  // a launch has fewer than 2^23 blocks
-  const int sub = UNITS == kWaves || wave < units ? unit / P.group : P.n_subs;
+  const int sub = UNITS == kWaves || wave < units ? unit / P.group : n_subs;
   const int h = g * P.group + unit % P.group;
   const long long qi = 32ll * sub + ql;
-  const bool in_range = qi < P.n_sel;
+  const bool in_range = qi < n_sel;
   int p = -1;
   long long row = -1;
-  if (in_range) {
+  if (PACKED && in_range) {
+    p = (int)qi;
+    row = row0 + qi;
+  } else if (in_range) {
     long long pp = P.q_pos[qi];
     row = P.q_rows ? (long long)P.q_rows[qi] : qi;
     if (row < 0 || row >= P.n_q_rows) { row = -1; pp = -1; }
@@ -186,8 +207,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   int pmax = -1;
   {
     const long long q_first = 32ll * (units * block / P.group);
-    const long long q_end = std::min<long long>(32ll * ((units * block + units - 1) / P.group + 1), P.n_sel);
-    for (long long q0 = q_first; q0 < q_end; q0 += 64) {
+    const long long q_end = std::min<long long>(32ll * ((units * block + units - 1) / P.group + 1), n_sel);
+    for (long long q0 = q_first; !PACKED && q0 < q_end; q0 += 64) {
       if (q0 + lane < q_end) {
         long long pp = P.q_pos[q0 + lane];
         if (pp > n_kv - 1) pp = n_kv - 1;
@@ -195,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       }
     }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) pmax = max(pmax, __shfl_xor(pmax, m));
+    for (int m = 32; !PACKED && m >= 1; m >>= 1) pmax = max(pmax, __shfl_xor(pmax, m));
     pmax = __builtin_amdgcn_readfirstlane(pmax);
   }
   uint4 qraw[8];
@@ -213,8 +234,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   pw_min = __builtin_amdgcn_readfirstlane(pw_min);  // equal in every lane: the mask test is scalar
   // this workgroup's share of the block's key tiles (all of them unless split)
   const int n_all = (pmax + kBN) / kBN;  // pmax = -1 -> 0 tiles
-  const int t0 = (int)((long long)n_all * split / P.n_split);
-  const int n_tiles = (int)((long long)n_all * (split + 1) / P.n_split) - t0;
+  const int t0 = PACKED ? item.tile0 : (int)((long long)n_all * split / P.n_split);
+  const int n_tiles = PACKED ? item.n_tiles : (int)((long long)n_all * (split + 1) / P.n_split) - t0;
 
   // Tiles go straight from HBM to LDS (buffer loads with an LDS destination:
   // lane l of an instruction writes 16 bytes at the wave's LDS address +
@@ -231,8 +252,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   //      transposing PV operand reads (4 rows x 4 pieces per half wave)
   //      fall in 16 distinct bank groups.
   const long long row_bytes = (long long)P.n_kv_heads * kHeadDim * 2;
-  const char* kbase = reinterpret_cast<const char*>(P.k);
-  const char* vbase = reinterpret_cast<const char*>(P.v);
+  const char* kbase = reinterpret_cast<const char*>(P.k) + row0 * row_bytes;
+  const char* vbase = reinterpret_cast<const char*>(P.v) + row0 * row_bytes;
   int koff[2], voff[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -374,7 +395,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
         const float p1 = __builtin_amdgcn_exp2f(fmaf(s[hf][k2 * 8 + 2 * e + 1], c2, -m_use));
         const f32x2 pv2 = {p0, p1};
         const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-        lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
+        if constexpr (PACKED) lt += p0 + p1;
+        else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
         w[e] = __builtin_bit_cast(uint32_t, pw);
       }
       pb2[k2] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
@@ -433,7 +455,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       const float p1 = __builtin_amdgcn_exp2f(x1);
       const f32x2 pv2 = {p0, p1};
       const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-      lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
+      if constexpr (PACKED) lt += p0 + p1;
+      else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
       w[k2][e] = __builtin_bit_cast(uint32_t, pw);
     }
   };
@@ -582,7 +605,22 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   const float l_tot = l_run + __shfl_xor(l_run, 32);
   if (!in_range) return;
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-  if (P.n_split > 1) {
+  if constexpr (PACKED) {
+    if (item.part >= 0) {
+      // a unit's place is full size: 16 x [half][query] pieces of 4 channels
+      const long long at = (((long long)item.part * P.n_kv_heads + g) * kWaves + wave) * 32;
+      float4* po = reinterpret_cast<float4*>(P.part_o + at * kHeadDim) + half * 32 + ql;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr)
+          po[(dt * 4 + rr) * 64] =
+              make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
+      if (half == 0) P.part_lse[at + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+      return;
+    }
+  }
+  if (!PACKED && P.n_split > 1) {
     const long long pair0 = ((long long)split * P.n_kv_heads + g) * P.n_sel * P.group + first_pair(P, unit);
     const int c = (int)std::min<long long>(32, P.n_sel - 32ll * sub);
     float4* po = reinterpret_cast<float4*>(P.part_o + pair0 * kHeadDim) + half * c + ql;
@@ -595,7 +633,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     if (half == 0) P.part_lse[pair0 + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
     return;
   }
-  uint16_t* op = P.out + (qi * P.n_q_heads + h) * (long long)kHeadDim + half * 4;
+  uint16_t* op = P.out + ((row0 + qi) * P.n_q_heads + h) * (long long)kHeadDim + half * 4;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -605,7 +643,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       *reinterpret_cast<uint2*>(op + dt * 32 + rr * 8) = make_uint2(w0, w1);
     }
   if (P.lse && half == 0)
-    P.lse[qi * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+    P.lse[(row0 + qi) * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
 }
 
 // Merge of the split partials of one unit's queries, one wave per 32 channels
@@ -666,6 +704,53 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(const Att
                                                         pack_bf16x2(a[rr * 4 + 2] * inv, a[rr * 4 + 3] * inv));
   if (P.lse && dt == 0 && half == 0)
     P.lse[qi * P.n_q_heads + h] = wsum > 0.f ? (m + log2f(wsum)) * 0.69314718055994531f : -INFINITY;
+}
+
+// The same for the packed sequences' blocks: parts joined in order, one wave
+// per 32 channels of a unit.
+__global__ __launch_bounds__(kCombineThreads) void pack_join_kernel(const AttnParams P) {
+  const int dt = threadIdx.x >> 6, lane = threadIdx.x & 63, ql = lane & 31, half = lane >> 5;
+  const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
+  const unsigned rest = blockIdx.x / (unsigned)P.n_kv_heads;
+  const int wave = (int)(rest % kWaves);
+  const PackJoin J = P.joins[rest / kWaves];
+  if (P.plan->id != P.plan_id) return;
+  const int unit = kWaves * J.block + wave;
+  const long long qi = 32ll * (unit / P.group) + ql;
+  const int h = g * P.group + unit % P.group;
+  if (qi >= J.len) return;
+  const long long stride = (long long)P.n_kv_heads * kWaves * 32;  // of a part
+  const long long at = (long long)J.first * stride + (g * kWaves + wave) * 32;
+  const float* lp = P.part_lse + at + ql;
+  const float4* po = reinterpret_cast<const float4*>(P.part_o + at * kHeadDim) + half * 32 + ql + dt * 4 * 64;
+  float m = -INFINITY;
+  for (int p = 0; p < J.n_parts; ++p) m = fmaxf(m, lp[p * stride]);
+  float a[16], wsum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) a[e] = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < J.n_parts; ++p) {
+    const float l = lp[p * stride];
+    // a part behind the query's last key holds nothing (zeros, -inf)
+    const float w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - m);
+    wsum += w;
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+      const float4 v = po[p * stride * (kHeadDim / 4) + rr * 64];
+      a[rr * 4] = fmaf(w, v.x, a[rr * 4]);
+      a[rr * 4 + 1] = fmaf(w, v.y, a[rr * 4 + 1]);
+      a[rr * 4 + 2] = fmaf(w, v.z, a[rr * 4 + 2]);
+      a[rr * 4 + 3] = fmaf(w, v.w, a[rr * 4 + 3]);
+    }
+  }
+  const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
+  uint16_t* op = P.out + ((J.row0 + qi) * P.n_q_heads + h) * (long long)kHeadDim + half * 4 + dt * 32;
+#pragma unroll
+  for (int rr = 0; rr < 4; ++rr)
+    *reinterpret_cast<uint2*>(op + rr * 8) = make_uint2(pack_bf16x2(a[rr * 4] * inv, a[rr * 4 + 1] * inv),
+                                                        pack_bf16x2(a[rr * 4 + 2] * inv, a[rr * 4 + 3] * inv));
+  if (P.lse && dt == 0 && half == 0)
+    P.lse[(J.row0 + qi) * P.n_q_heads + h] = wsum > 0.f ? (m + log2f(wsum)) * 0.69314718055994531f : -INFINITY;
 }
 
 hipError_t launch_combine(const AttnParams& P, hipStream_t s) {
@@ -791,6 +876,38 @@ hipError_t launch_attention(const uint16_t* q, int64_t n_q_rows, const int32_t* 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp == 1) return e;
   return launch_combine(P, s);
+}
+
+hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_joins, int n_parts,
+                                   const uint16_t* q, const uint16_t* k, const uint16_t* v, int n_q_heads,
+                                   int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws, hipStream_t s) {
+  if (n_items <= 0) return hipSuccess;
+  AttnParams P = {};
+  P.q = q;
+  P.k = k;
+  P.v = v;
+  P.n_q_heads = n_q_heads;
+  P.n_kv_heads = n_kv_heads;
+  P.group = n_q_heads / n_kv_heads;
+  P.scale_log2 = scale * 1.4426950408889634f;
+  P.out = out;
+  P.lse = lse;
+  P.n_split = 1;
+  P.units = kWaves;
+  const char* base = static_cast<const char*>(plan);
+  P.plan = reinterpret_cast<const PackHeader*>(base);
+  P.items = reinterpret_cast<const PackItem*>(base + pack_items_offset());
+  P.joins = reinterpret_cast<const PackJoin*>(base + pack_joins_offset(n_items));
+  P.plan_id = id;
+  P.part_o = static_cast<float*>(ws);
+  P.part_lse = P.part_o + (size_t)n_parts * n_kv_heads * kWaves * 32 * kHeadDim;
+  hipLaunchKernelGGL((sparse_attn_kernel<kWaves, true>), dim3((unsigned)n_items * (unsigned)n_kv_heads), dim3(kThreads),
+                     0, s, P);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || n_joins == 0) return e;
+  hipLaunchKernelGGL(pack_join_kernel, dim3((unsigned)n_joins * kWaves * (unsigned)n_kv_heads), dim3(kCombineThreads), 0,
+                     s, P);
+  return hipGetLastError();
 }
 
 }  // namespace kvc

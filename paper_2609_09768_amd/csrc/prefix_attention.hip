@@ -1,0 +1,513 @@
+// Attention of a batch over one shared prefix and over rows of their own
+// (gfx950).
+//
+// Sequence s has n_new query tokens at the end of its own rows 0 .. len - 1,
+// which lie in pages of a pool and follow a prefix that all sequences share
+// (the blended context).  Query i sees the whole prefix and its own rows 0 ..
+// t = len - n_new + i:
+//   O = softmax_j(scale * <q, k_j>) v_j  over prefix and own rows together.
+// A softmax over a union is the weighted mean of the softmaxes over its
+// parts, with weights e^(lse of the part), so the key axis is cut into parts
+// that are computed apart and joined by a last kernel in a fixed order:
+// the prefix into shares of its key tiles, each read once for ALL rows
+// (sequence, token, query head of the group) of a kv head, and every
+// sequence's own rows into chunks.
+//
+// With few rows this is bound by the bytes of K and V: 512 per key and kv head
+// against 4 x 128 FLOP per row.  So the kernel is built around loads in
+// flight.  A workgroup has four waves, one per SIMD; each takes every fourth
+// 32-key tile of the part by itself, with two LDS slots of its own that loads
+// fill without registers (16 KB each, so 64 to 128 KB per CU under way)
+// and no barrier until the waves join their results.  The matrix work of a
+// tile (v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T, a lane holds
+// one row and 16 of the keys) takes 512 cycles for 32 rows, against about
+// 1,500 for a CU's share of HBM to bring its 16 KB; up to two units of 32
+// rows share each tile in registers (four do not fit them).
+// Scores, softmax and sums are float32 (the sums of the unrounded weights, so
+// the log-sum is exact to float32); weights are rounded to bf16 for the product
+// with V, whose operand they are: each is off by 2^-8 of itself at most, and
+// the output is rounded to as many bits.
+#include <algorithm>
+
+#include "bf16_util.h"
+#include "kvc_internal.h"
+
+namespace kvc {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+typedef __attribute__((address_space(1))) const void global_void;
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kTile = 32;                       // keys of a tile
+constexpr int kKGroup = 4 * kHeadDim + 32;      // bf16 per four K rows in LDS (1088 B, spreads the banks)
+constexpr int kKSlot = (kTile / 4) * kKGroup;   // of one wave
+constexpr int kVSlot = kTile * kHeadDim;
+constexpr int kMaxIds = 1024;                   // page numbers a workgroup keeps in LDS
+
+// What rows that are not there are loaded as.
+__device__ const uint4 zero_row[16] = {};
+
+struct PrefixParams {
+  const uint16_t* q;
+  int n_new, n_slots, n_q_heads, n_kv_heads, group;
+  int rows;        // of a kv head: n_slots x n_new x group
+  int slot_rows;   // of a slot: n_new x group
+  const uint16_t* kp;
+  const uint16_t* vp;
+  int n_prefix;
+  const uint16_t* kt;
+  const uint16_t* vt;
+  PageTables pages;
+  float scale_log2;
+  int prefix_parts, prefix_blocks;  // shares of the prefix, blocks of rows
+  int own_parts, own_blocks, chunk; // chunks of a slot's rows (chunk rows each), blocks of rows
+  float* part_o;    // [part][kv head][row][D], parts of the prefix first
+  float* part_lse;  // [part][kv head][row], log2
+  uint16_t* out;
+  float* lse;
+};
+
+__device__ __forceinline__ bf16x8 as_bf16x8(const uint4& u) { return __builtin_bit_cast(bf16x8, u); }
+__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+
+// UNITS: groups of 32 rows that share the tiles.
+template <int UNITS>
+__global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixParams P) {
+  // one array per slot, so that alias analysis can tell a slot being loaded
+  // from the one being read; each wave has its own part of them
+  __shared__ __attribute__((aligned(16))) uint16_t K0[kWaves * kKSlot], K1[kWaves * kKSlot];
+  __shared__ __attribute__((aligned(16))) uint16_t V0[kWaves * kVSlot], V1[kWaves * kVSlot];
+  __shared__ int ids[kMaxIds];
+  __shared__ float wm[kWaves][32], wl[kWaves][32];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ql = lane & 31, half = lane >> 5;
+
+  // this workgroup's part of the keys and block of rows
+  const unsigned hkv = (unsigned)P.n_kv_heads;
+  const int g = (int)(blockIdx.x % hkv);
+  unsigned rest = blockIdx.x / hkv;
+  const unsigned n_prefix_wgs = (unsigned)P.prefix_parts * (unsigned)P.prefix_blocks;
+  const bool own = rest >= n_prefix_wgs;
+  int part, row0, row_end, key0, key_end, slot = 0, have = 0;
+  if (!own) {
+    const int rb = (int)(rest % (unsigned)P.prefix_blocks);
+    part = (int)(rest / (unsigned)P.prefix_blocks);
+    row0 = rb * (32 * UNITS);
+    row_end = P.rows;
+    const long long tiles = ((long long)P.n_prefix + kTile - 1) / kTile;
+    key0 = (int)(tiles * part / P.prefix_parts) * kTile;
+    key_end = min((int)std::min<long long>(tiles * (part + 1) / P.prefix_parts * kTile, P.n_prefix), P.n_prefix);
+  } else {
+    rest -= n_prefix_wgs;
+    const int rb = (int)(rest % (unsigned)P.own_blocks);
+    rest /= (unsigned)P.own_blocks;
+    slot = (int)(rest % (unsigned)P.n_slots);
+    const int c = (int)(rest / (unsigned)P.n_slots);
+    have = min(max(P.pages.len[slot], 0), P.pages.max_pages << P.pages.page_shift);
+    key0 = c * P.chunk;
+    if (key0 >= have) return;  // every wave: nothing of this chunk is there, and the join knows it
+    key_end = (int)std::min<long long>((long long)key0 + P.chunk, have);
+    part = P.prefix_parts + c;
+    row0 = slot * P.slot_rows + rb * (32 * UNITS);
+    row_end = (slot + 1) * P.slot_rows;
+    // the chunk's pages; an entry outside the pool has no rows
+    const int first = key0 >> P.pages.page_shift;
+    const int n_ids = ((key_end - 1) >> P.pages.page_shift) - first + 1;
+    for (int i = tid; i < n_ids; i += kThreads) {
+      const int p = P.pages.table[(size_t)slot * P.pages.max_pages + first + i];
+      ids[i] = p >= 0 && p < P.pages.n_pages ? p : -1;
+    }
+  }
+
+  // queries of the rows, and how many keys of the tensor each row sees
+  bf16x8 qreg[UNITS][8];
+  int sees[UNITS];
+  int sees_least = 0x7fffffff;
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    const int r = row0 + 32 * u + ql;
+    const bool in = r < row_end;
+    const int tok = r / P.group;
+    const uint16_t* qp =
+        P.q + ((long long)tok * P.n_q_heads + g * P.group + (r - tok * P.group)) * kHeadDim + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+      qreg[u][ks] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(qp + ks * 16) : make_uint4(0, 0, 0, 0));
+    sees[u] = own ? max(have - P.n_new + (tok - slot * P.n_new) + 1, 0) : P.n_prefix;
+    if (in) sees_least = min(sees_least, sees[u]);
+  }
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) sees_least = min(sees_least, __shfl_xor(sees_least, m));
+  sees_least = __builtin_amdgcn_readfirstlane(sees_least);
+  const int units = min(UNITS, (row_end - row0 + 31) / 32);
+  __syncthreads();  // ids
+
+  // A tile: eight loads of four rows of K, then eight of V; lane l of a load
+  // fills 16 bytes at the wave's LDS address + 16 l.  LDS pieces are swizzled
+  // for the operand reads: K row r's piece p at p ^ (r & 3), V's at
+  // p ^ 4 (r & 3).
+  const long long row_bytes = (long long)P.n_kv_heads * kHeadDim * 2;
+  const int lr = lane >> 4, lp = lane & 15;
+  const int k_piece = 16 * (lp ^ lr), v_piece = 16 * (lp ^ (4 * lr));
+  const char* zero = reinterpret_cast<const char*>(zero_row);
+  auto issue = [&](int k0, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
+    long long at[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int key = k0 + 4 * j + lr;
+      at[j] = -1;
+      if (key < key_end) {
+        long long r = key;
+        if (own) {
+          const int p = ids[(key >> P.pages.page_shift) - (key0 >> P.pages.page_shift)];
+          r = p < 0 ? -1 : ((long long)p << P.pages.page_shift) + (key & ((1 << P.pages.page_shift) - 1));
+        }
+        if (r >= 0) at[j] = r * row_bytes + g * (kHeadDim * 2);
+      }
+    }
+    const char* kb = reinterpret_cast<const char*>(own ? P.kt : P.kp);
+    const char* vb = reinterpret_cast<const char*>(own ? P.vt : P.vp);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* from = (at[j] >= 0 ? kb + at[j] : zero) + k_piece;
+      __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)(ks_ + j * kKGroup), 16, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* from = (at[j] >= 0 ? vb + at[j] : zero) + v_piece;
+      __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)(vs_ + 4 * j * kHeadDim), 16, 0, 0);
+    }
+  };
+  // Whether any of the pages is outside the pool: its keys are masked like
+  // keys past the end.
+  int gaps = 0;
+  if (own) {
+    for (int i = lane; i <= ((key_end - 1) >> P.pages.page_shift) - (key0 >> P.pages.page_shift); i += 64)
+      gaps |= ids[i] < 0;
+    gaps = __any(gaps);
+  }
+
+  // operand reads: A = K rows lane % 32, dims 16 ks + 8 half .. + 8; and
+  // A = V^T, dims 32 dt + lane % 32, keys in the order in which the S^T
+  // accumulator holds them (8 (e / 4) + 4 half + e % 4), by transposing reads
+  const int k_a0 = (ql >> 2) * kKGroup + (lane & 3) * kHeadDim + 8 * (half ^ (lane & 1));
+  const int k_e1 = 16 * ((lane >> 1) & 1);
+  const int k_rd[2] = {k_a0 + k_e1, k_a0 - k_e1};
+  int v_rd[4];
+  {
+    const int i = lane & 15, gd = (lane >> 4) & 1, sr = i >> 2;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+      v_rd[dt] = (4 * half + sr) * kHeadDim + 32 * (dt ^ sr) + 16 * gd + 4 * (i & 3);
+  }
+
+  f32x16 o[UNITS][4];
+  float m_run[UNITS], l_run[UNITS];
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    m_run[u] = -INFINITY;
+    l_run[u] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[u][dt][r] = 0.f;
+  }
+
+  auto tile = [&](int k0, const uint16_t* ks_, const uint16_t* vs_, auto&& wait_v) __attribute__((always_inline)) {
+    uint4 kf[8];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) kf[ks] = *reinterpret_cast<const uint4*>(ks_ + k_rd[ks & 1] + 16 * ks);
+    bf16x8 pb[UNITS][2];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      if (u >= units) break;
+      f32x16 s = {};
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[ks]), qreg[u][ks], s, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] *= P.scale_log2;
+      if (k0 + kTile > sees_least || k0 + kTile > key_end || gaps) {
+        // first key that is not seen, for each four keys of the lane (which
+        // share a page); as plain selects, no branch inside the unit
+        const int limit = min(sees[u], key_end);
+        int lim[4] = {limit, limit, limit, limit};
+        if (gaps) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = min(k0 + 8 * j + half * 4, key_end - 1);
+            const int id = ids[(key >> P.pages.page_shift) - (key0 >> P.pages.page_shift)];
+            lim[j] = id < 0 ? key0 : limit;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[r] = k0 + (r >> 2) * 8 + half * 4 + (r & 3) >= lim[r >> 2] ? -INFINITY : s[r];
+      }
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      const float m_new = fmaxf(m_run[u], fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run[u] - m_use);
+      if (__any(m_new > m_run[u])) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[u][dt][r] *= alpha;
+      }
+      m_run[u] = m_new;
+      float sum = 0.f;
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(s[2 * e] - m_use), p1 = __builtin_amdgcn_exp2f(s[2 * e + 1] - m_use);
+        sum += p0 + p1;
+        w[e] = pack_bf16x2(p0, p1);
+      }
+      l_run[u] = fmaf(l_run[u], alpha, sum);
+      pb[u][0] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+      pb[u][1] = as_bf16x8(make_uint4(w[4], w[5], w[6], w[7]));
+    }
+    wait_v();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int kk = i >> 2, dt = i & 3;
+      const uint16_t* b = vs_ + v_rd[dt] + kk * 16 * kHeadDim;
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b + 8 * kHeadDim));
+      const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+      const bf16x8 vf = as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y));
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        if (u >= units) break;
+        o[u][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[u][kk], o[u][dt], 0, 0, 0);
+      }
+    }
+  };
+
+  // Tile i of this wave starts at key0 + 32 (4 i + wave) and goes to slot i %
+  // 2.  Loads return in order: with the next tile's 16 under way, K is there
+  // when at most 24 are left, V when at most 16 are.
+  const int n_all = (key_end - key0 + kTile - 1) / kTile;
+  const int n = n_all > wave ? (n_all - wave + kWaves - 1) / kWaves : 0;
+  auto start = [&](int i) __attribute__((always_inline)) { return key0 + kTile * (kWaves * i + wave); };
+  uint16_t* const ks0 = K0 + wave * kKSlot;
+  uint16_t* const ks1 = K1 + wave * kKSlot;
+  uint16_t* const vs0 = V0 + wave * kVSlot;
+  uint16_t* const vs1 = V1 + wave * kVSlot;
+  auto step = [&](int i, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
+    const bool more = i + 1 < n;  // the same in every lane
+    if (more) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    tile(start(i), ks_, vs_, [&]() __attribute__((always_inline)) {
+      if (more) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    });
+    if (i + 2 < n) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+      issue(start(i + 2), ks_, vs_);
+    }
+  };
+  // the queries' loads are done before the count of loads under way begins
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (n > 0) issue(start(0), ks0, vs0);
+  if (n > 1) issue(start(1), ks1, vs1);
+  for (int i = 0; i < n; i += 2) {
+    step(i, ks0, vs0);
+    if (i + 1 < n) step(i + 1, ks1, vs1);
+  }
+
+  // join the waves, half the channels of a unit at a time (32 KB of LDS),
+  // in wave order
+  float4* const red = reinterpret_cast<float4*>(K0);
+  static_assert(sizeof(K0) >= kWaves * 8 * 64 * sizeof(float4), "the waves' sums of half the channels");
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    if (u >= units) break;
+    const float l_tot = l_run[u] + __shfl_xor(l_run[u], 32);
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      __syncthreads();
+      if (half == 0 && hf == 0) {
+        wm[wave][ql] = m_run[u];
+        wl[wave][ql] = l_tot;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const f32x16& a = o[u][2 * hf + (e >> 2)];
+        const int rr = 4 * (e & 3);
+        red[(wave * 8 + e) * 64 + lane] = make_float4(a[rr], a[rr + 1], a[rr + 2], a[rr + 3]);
+      }
+      __syncthreads();
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wm[w][ql]);
+      float l = 0.f, f[kWaves];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        f[w] = wm[w][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][ql] - m);
+        l = fmaf(f[w], wl[w][ql], l);
+      }
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const int r = row0 + 32 * u + ql;
+      const long long at = ((long long)part * P.n_kv_heads + g) * P.rows + r;
+#pragma unroll
+      for (int e2 = 0; e2 < 2; ++e2) {
+        const int e = 2 * wave + e2;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float4 x = red[(w * 8 + e) * 64 + lane];
+          a.x = fmaf(f[w], x.x, a.x);
+          a.y = fmaf(f[w], x.y, a.y);
+          a.z = fmaf(f[w], x.z, a.z);
+          a.w = fmaf(f[w], x.w, a.w);
+        }
+        if (r < row_end)
+          *reinterpret_cast<float4*>(P.part_o + at * kHeadDim + 64 * hf + 32 * (e >> 2) + 8 * (e & 3) + 4 * half) =
+              make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+      }
+      if (hf == 0 && wave == 0 && half == 0 && r < row_end) P.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
+    }
+  }
+}
+
+// Joins the parts of a row, one wave per row and head (two channels a lane),
+// in the order of the parts: weights 2^(lse - max).
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixParams P) {
+  const int lane = threadIdx.x & 63;
+  const long long i = (long long)blockIdx.x * (kJoinThreads / 64) + (threadIdx.x >> 6);
+  if (i >= (long long)P.rows * P.n_kv_heads) return;
+  const int g = (int)(i / P.rows), r = (int)(i - (long long)g * P.rows);
+  const int tok = r / P.group, h = g * P.group + (r - tok * P.group), slot = tok / P.n_new;
+  const int have = min(max(P.pages.len[slot], 0), P.pages.max_pages << P.pages.page_shift);
+  const int t = have - P.n_new + (tok - slot * P.n_new);  // its place among the slot's rows
+  const int own = t < 0 ? 0 : (int)(((long long)have + P.chunk - 1) / P.chunk);
+  const int parts = t < 0 ? 0 : P.prefix_parts + own;
+  const long long stride = (long long)P.n_kv_heads * P.rows;
+  const float* lp = P.part_lse + (long long)g * P.rows + r;
+  const float* op = P.part_o + ((long long)g * P.rows + r) * kHeadDim + 2 * lane;
+  float m = -INFINITY;
+  for (int p = lane; p < parts; p += 64) m = fmaxf(m, lp[p * stride]);
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+  float a = 0.f, b = 0.f, sum = 0.f;
+  if (m != -INFINITY) {
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+      const float w = __builtin_amdgcn_exp2f(lp[p * stride] - m);
+      const float2 x = *reinterpret_cast<const float2*>(op + p * stride * kHeadDim);
+      a = fmaf(w, x.x, a);
+      b = fmaf(w, x.y, b);
+      sum += w;
+    }
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const long long at = (long long)tok * P.n_q_heads + h;
+  *reinterpret_cast<uint32_t*>(P.out + at * kHeadDim + 2 * lane) = pack_bf16x2(a * inv, b * inv);
+  if (P.lse && lane == 0) P.lse[at] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+}
+
+long long div_up(long long a, long long b) { return (a + b - 1) / b; }
+
+constexpr int kCus = 256;
+
+// How a call is cut.  Units of 32 rows that share a tile: as many as the rows
+// fill, up to two.  The prefix in as many shares as give every CU a
+// workgroup, each wave of it at least one tile; a slot's rows in chunks of
+// 512 (four tiles a wave) unless its table holds more than 32 of them.
+struct Cut {
+  int units, prefix_parts, prefix_blocks, own_parts, own_blocks, chunk;
+};
+Cut cut(int64_t n_prefix, int64_t rows, int64_t slot_rows, int n_kv_heads, int page_rows, int max_pages) {
+  Cut c;
+  c.units = rows <= 32 ? 1 : 2;
+  c.prefix_blocks = (int)div_up(rows, 32 * c.units);
+  const long long tiles = div_up(n_prefix, kTile);
+  c.prefix_parts = n_prefix == 0 || rows == 0 ? 0
+                                 : (int)std::max<long long>(1, std::min<long long>(div_up(kCus, (long long)n_kv_heads * c.prefix_blocks),
+                                                                                  div_up(tiles, kWaves)));
+  const long long most = (long long)max_pages * page_rows;
+  c.chunk = (int)std::min<long long>(std::max<long long>(512, div_up(most, 32 * 128) * 128), (long long)kMaxIds * page_rows);
+  c.own_parts = (int)div_up(most, c.chunk);
+  c.own_blocks = (int)div_up(slot_rows, 32 * c.units);
+  return c;
+}
+
+}  // namespace
+
+size_t prefix_attention_ws_bytes(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
+                                 int page_rows, int max_pages) {
+  const int64_t slot_rows = (int64_t)n_new * (n_q_heads / n_kv_heads), rows = slot_rows * n_slots;
+  const Cut c = cut(n_prefix, rows, slot_rows, n_kv_heads, page_rows, max_pages);
+  return align256(size_t(c.prefix_parts + c.own_parts) * size_t(n_kv_heads) * size_t(rows) * (kHeadDim + 1) * sizeof(float));
+}
+
+int64_t prefix_attention_workgroups(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
+                                    int page_rows, int max_pages) {
+  const int64_t slot_rows = (int64_t)n_new * (n_q_heads / n_kv_heads), rows = slot_rows * n_slots;
+  const Cut c = cut(n_prefix, rows, slot_rows, n_kv_heads, page_rows, max_pages);
+  return ((int64_t)c.prefix_parts * c.prefix_blocks + (int64_t)c.own_parts * c.own_blocks * n_slots) * n_kv_heads;
+}
+
+hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t* kp, const uint16_t* vp,
+                                   int64_t n_prefix, const PageTables& pages, const uint16_t* kt, const uint16_t* vt,
+                                   int n_q_heads, int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws,
+                                   hipStream_t s) {
+  PrefixParams P;
+  P.q = q;
+  P.n_new = n_new;
+  P.n_slots = pages.n_slots;
+  P.n_q_heads = n_q_heads;
+  P.n_kv_heads = n_kv_heads;
+  P.group = n_q_heads / n_kv_heads;
+  P.slot_rows = n_new * P.group;
+  P.rows = P.slot_rows * P.n_slots;
+  P.kp = kp;
+  P.vp = vp;
+  P.n_prefix = (int)n_prefix;
+  P.kt = kt;
+  P.vt = vt;
+  P.pages = pages;
+  P.scale_log2 = scale * 1.4426950408889634f;
+  const Cut c = cut(n_prefix, P.rows, P.slot_rows, n_kv_heads, 1 << pages.page_shift, pages.max_pages);
+  P.prefix_parts = c.prefix_parts;
+  P.prefix_blocks = c.prefix_blocks;
+  P.own_parts = c.own_parts;
+  P.own_blocks = c.own_blocks;
+  P.chunk = c.chunk;
+  P.part_o = static_cast<float*>(ws);
+  P.part_lse = P.part_o + (size_t)(c.prefix_parts + c.own_parts) * n_kv_heads * P.rows * kHeadDim;
+  P.out = out;
+  P.lse = lse;
+  const long long wgs = ((long long)c.prefix_parts * c.prefix_blocks + (long long)c.own_parts * c.own_blocks * P.n_slots) * n_kv_heads;
+  if (wgs > 0) {
+    const dim3 grid((unsigned)wgs), block(kThreads);
+    if (c.units == 1) hipLaunchKernelGGL(prefix_attn_kernel<1>, grid, block, 0, s, P);
+    else hipLaunchKernelGGL(prefix_attn_kernel<2>, grid, block, 0, s, P);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const long long waves = (long long)P.rows * n_kv_heads;
+  hipLaunchKernelGGL(prefix_join_kernel, dim3((unsigned)div_up(waves, kJoinThreads / 64)), dim3(kJoinThreads), 0, s, P);
+  return hipGetLastError();
+}
+
+}  // namespace kvc
