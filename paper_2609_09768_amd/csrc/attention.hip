@@ -147,12 +147,15 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
 
 // UNITS: units of a workgroup, 0 where only P.units says (which costs 0.4 us
 // before the first loads, of the 31 of a check layer of 1,024 rows).
-// PACKED: every query of many sequences that lie back to back, causal inside
+// kPacked: every query of many sequences that lie back to back, causal inside
 // each (chunks prefilled on their own).  Blocks, their order and their shares
 // of the key tiles come from the plan's work items; the rest is the same.
-// The weights' sums are taken before they are rounded to bf16, one more
-// addition per pair, which makes the log-sum exact to float32.
-template <int UNITS, bool PACKED = false>
+// kPrefix: rows (token, head of the group) of a kv head that all see every key
+// (a batch over one shared prefix); a unit is 32 of them.
+// In both the weights' sums are taken before they are rounded to bf16, one
+// more addition per pair, which makes the log-sum exact to float32.
+enum class Rows { kSelected, kPacked, kPrefix };
+template <int UNITS, Rows ROWS = Rows::kSelected>
 __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams P) {
   // one array per slot, so alias analysis can tell a slot being loaded
   // from the slots being read
@@ -170,13 +173,17 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 
   const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
   const unsigned rest = blockIdx.x / (unsigned)P.n_kv_heads;
+  constexpr bool PACKED = ROWS == Rows::kPacked, PREFIX = ROWS == Rows::kPrefix;
   PackItem item = {};
   if constexpr (PACKED) {
     item = P.items[rest];
     if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
   }
-  const int split = PACKED ? 0 : (int)(rest % (unsigned)P.n_split);
-  const int block = PACKED ? item.block : P.n_blocks - 1 - (int)(rest / (unsigned)P.n_split);
+  // (of a prefix, blocks of rows run together through the same keys)
+  const int split = PACKED ? 0 : PREFIX ? (int)(rest / (unsigned)P.n_blocks) : (int)(rest % (unsigned)P.n_split);
+  const int block = PACKED   ? item.block
+                    : PREFIX ? (int)(rest % (unsigned)P.n_blocks)
+                             : P.n_blocks - 1 - (int)(rest / (unsigned)P.n_split);
   const long long n_kv = PACKED ? item.len : P.n_kv;
   const long long n_sel = PACKED ? item.len : P.n_sel;
   const int n_subs = PACKED ? (item.len + 31) / 32 : P.n_subs;
@@ -186,8 +193,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   // past the workgroup's units has none, like the units past the last group
   const int units = UNITS ? UNITS : P.units;
   const int unit = units * block + wave;  // a launch has fewer than 2^23 blocks
-  const int sub = UNITS == kWaves || wave < units ? unit / P.group : n_subs;
-  const int h = g * P.group + unit % P.group;
+  const int sub = PREFIX ? unit : UNITS == kWaves || wave < units ? unit / P.group : n_subs;
+  int h = g * P.group + unit % P.group;
   const long long qi = 32ll * sub + ql;
   const bool in_range = qi < n_sel;
   int p = -1;
@@ -195,6 +202,10 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   if (PACKED && in_range) {
     p = (int)qi;
     row = row0 + qi;
+  } else if (PREFIX && in_range) {
+    p = (int)n_kv - 1;
+    row = qi / P.group;
+    h = g * P.group + (int)(qi - row * P.group);
   } else if (in_range) {
     long long pp = P.q_pos[qi];
     row = P.q_rows ? (long long)P.q_rows[qi] : qi;
@@ -208,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   {
     const long long q_first = 32ll * (units * block / P.group);
     const long long q_end = std::min<long long>(32ll * ((units * block + units - 1) / P.group + 1), n_sel);
-    for (long long q0 = q_first; !PACKED && q0 < q_end; q0 += 64) {
+    for (long long q0 = q_first; ROWS == Rows::kSelected && q0 < q_end; q0 += 64) {
       if (q0 + lane < q_end) {
         long long pp = P.q_pos[q0 + lane];
         if (pp > n_kv - 1) pp = n_kv - 1;
@@ -216,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       }
     }
 #pragma unroll
-    for (int m = 32; !PACKED && m >= 1; m >>= 1) pmax = max(pmax, __shfl_xor(pmax, m));
+    for (int m = 32; ROWS == Rows::kSelected && m >= 1; m >>= 1) pmax = max(pmax, __shfl_xor(pmax, m));
     pmax = __builtin_amdgcn_readfirstlane(pmax);
   }
   uint4 qraw[8];
@@ -233,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   for (int m = 32; m >= 1; m >>= 1) pw_min = min(pw_min, __shfl_xor(pw_min, m));
   pw_min = __builtin_amdgcn_readfirstlane(pw_min);  // equal in every lane: the mask test is scalar
   // this workgroup's share of the block's key tiles (all of them unless split)
-  const int n_all = (pmax + kBN) / kBN;  // pmax = -1 -> 0 tiles
+  const int n_all = PREFIX ? (int)((n_kv + kBN - 1) / kBN) : (pmax + kBN) / kBN;  // pmax = -1 -> 0 tiles
   const int t0 = PACKED ? item.tile0 : (int)((long long)n_all * split / P.n_split);
   const int n_tiles = PACKED ? item.n_tiles : (int)((long long)n_all * (split + 1) / P.n_split) - t0;
 
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
         const float p1 = __builtin_amdgcn_exp2f(fmaf(s[hf][k2 * 8 + 2 * e + 1], c2, -m_use));
         const f32x2 pv2 = {p0, p1};
         const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-        if constexpr (PACKED) lt += p0 + p1;
+        if constexpr (ROWS != Rows::kSelected) lt += p0 + p1;
         else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
         w[e] = __builtin_bit_cast(uint32_t, pw);
       }
@@ -455,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       const float p1 = __builtin_amdgcn_exp2f(x1);
       const f32x2 pv2 = {p0, p1};
       const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-      if constexpr (PACKED) lt += p0 + p1;
+      if constexpr (ROWS != Rows::kSelected) lt += p0 + p1;
       else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
       w[k2][e] = __builtin_bit_cast(uint32_t, pw);
     }
@@ -619,6 +630,18 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       if (half == 0) P.part_lse[at + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
       return;
     }
+  }
+  if constexpr (PREFIX) {
+    const long long at = ((long long)split * P.n_kv_heads + g) * n_sel + qi;
+    float* po = P.part_o + at * kHeadDim + half * 4;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        *reinterpret_cast<float4*>(po + dt * 32 + rr * 8) =
+            make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
+    if (half == 0) P.part_lse[at] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+    return;
   }
   if (!PACKED && P.n_split > 1) {
     const long long pair0 = ((long long)split * P.n_kv_heads + g) * P.n_sel * P.group + first_pair(P, unit);
@@ -901,12 +924,36 @@ hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, i
   P.plan_id = id;
   P.part_o = static_cast<float*>(ws);
   P.part_lse = P.part_o + (size_t)n_parts * n_kv_heads * kWaves * 32 * kHeadDim;
-  hipLaunchKernelGGL((sparse_attn_kernel<kWaves, true>), dim3((unsigned)n_items * (unsigned)n_kv_heads), dim3(kThreads),
+  hipLaunchKernelGGL((sparse_attn_kernel<kWaves, Rows::kPacked>), dim3((unsigned)n_items * (unsigned)n_kv_heads), dim3(kThreads),
                      0, s, P);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || n_joins == 0) return e;
   hipLaunchKernelGGL(pack_join_kernel, dim3((unsigned)n_joins * kWaves * (unsigned)n_kv_heads), dim3(kCombineThreads), 0,
                      s, P);
+  return hipGetLastError();
+}
+
+hipError_t launch_prefix_rows(const uint16_t* q, int64_t rows, int n_q_heads, int n_kv_heads, const uint16_t* k,
+                              const uint16_t* v, int64_t n_kv, int parts, float scale, float* part_o, float* part_lse,
+                              hipStream_t s) {
+  AttnParams P = {};
+  P.q = q;
+  P.k = k;
+  P.v = v;
+  P.n_sel = rows;
+  P.n_kv = n_kv;
+  P.n_q_heads = n_q_heads;
+  P.n_kv_heads = n_kv_heads;
+  P.group = n_q_heads / n_kv_heads;
+  P.n_subs = (int)div_up(rows, 32);
+  P.n_blocks = (int)div_up(P.n_subs, kWaves);
+  P.scale_log2 = scale * 1.4426950408889634f;
+  P.n_split = parts;
+  P.units = kWaves;
+  P.part_o = part_o;
+  P.part_lse = part_lse;
+  hipLaunchKernelGGL((sparse_attn_kernel<kWaves, Rows::kPrefix>),
+                     dim3((unsigned)parts * (unsigned)P.n_blocks * (unsigned)n_kv_heads), dim3(kThreads), 0, s, P);
   return hipGetLastError();
 }
 

@@ -199,6 +199,13 @@ hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t*
                                    int n_q_heads, int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws,
                                    hipStream_t s);
 
+// Its prefix for many rows (attention.hip): parts shares of the keys, results
+// [part][kv head][row][D] and [part][kv head][row] (log2), where row r of kv
+// head g is head g G + r % G of token r / G.
+hipError_t launch_prefix_rows(const uint16_t* q, int64_t rows, int n_q_heads, int n_kv_heads, const uint16_t* k,
+                              const uint16_t* v, int64_t n_kv, int parts, float scale, float* part_o, float* part_lse,
+                              hipStream_t s);
+
 // ---- packed sequences (attention.hip) -----------------------------------------------
 // Work of one workgroup and kv head: eight units (32 queries of one head each)
 // of one sequence over key tiles tile0 .. tile0 + n_tiles - 1.  part: where

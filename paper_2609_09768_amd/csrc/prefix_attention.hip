@@ -13,16 +13,18 @@
 // (sequence, token, query head of the group) of a kv head, and every
 // sequence's own rows into chunks.
 //
-// With few rows this is bound by the bytes of K and V: 512 per key and kv head
-// against 4 x 128 FLOP per row.  So the kernel is built around loads in
-// flight.  A workgroup has four waves, one per SIMD; each takes every fourth
-// 32-key tile of the part by itself, with two LDS slots of its own that loads
-// fill without registers (16 KB each, so 64 to 128 KB per CU under way)
-// and no barrier until the waves join their results.  The matrix work of a
-// tile (v_mfma_f32_32x32x16_bf16: S^T = K Q^T, O^T += V^T P^T, a lane holds
-// one row and 16 of the keys) takes 512 cycles for 32 rows, against about
-// 1,500 for a CU's share of HBM to bring its 16 KB; up to two units of 32
-// rows share each tile in registers (four do not fit them).
+// Up to 32 rows of a kv head are bound by the bytes of K and V: 512 per key
+// and kv head against 4 x 128 FLOP per row.  So the kernel here is built
+// around loads in flight.  A workgroup has eight waves, two per SIMD; each
+// takes every eighth 32-key tile of the part by itself, with a K slot and a V
+// slot of its own in LDS that loads fill without registers: the next K tile is
+// asked for when the scores are done, the next V tile when the product is, so
+// 64 to 128 KB per CU are under way, and no barrier is met until the waves join
+// their results.  The matrix work of a tile (v_mfma_f32_32x32x16_bf16: S^T = K
+// Q^T, O^T += V^T P^T, a lane holds one row and 16 of the keys) takes 512
+// cycles, against about 1,500 for a CU's share of HBM to bring its 16 KB.
+// More rows go to the kernel of the other attentions (attention.hip), whose
+// eight waves of 32 rows share every tile.
 // Scores, softmax and sums are float32 (the sums of the unrounded weights, so
 // the log-sum is exact to float32); weights are rounded to bf16 for the product
 // with V, whose operand they are: each is off by 2^-8 of itself at most, and
@@ -44,13 +46,18 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 typedef __attribute__((address_space(1))) const void global_void;
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 32;                       // keys of a tile
 constexpr int kKGroup = 4 * kHeadDim + 32;      // bf16 per four K rows in LDS (1088 B, spreads the banks)
 constexpr int kKSlot = (kTile / 4) * kKGroup;   // of one wave
 constexpr int kVSlot = kTile * kHeadDim;
-constexpr int kMaxIds = 1024;                   // page numbers a workgroup keeps in LDS
+constexpr int kMaxIds = 64;                     // pages of a chunk: one a lane
+// s_waitcnt immediates (vmcnt bits 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8) as
+// the builtin takes them, which the compiler's own wait counting understands:
+// at most n vector loads under way; LDS reads done.
+constexpr int wait_vm(int n) { return (n & 15) | (n >> 4) << 14 | 7 << 4 | 15 << 8; }
+constexpr int kWaitLds = 15 | 3 << 14 | 7 << 4;
 
 // What rows that are not there are loaded as.
 __device__ const uint4 zero_row[16] = {};
@@ -68,6 +75,7 @@ struct PrefixParams {
   PageTables pages;
   float scale_log2;
   int prefix_parts, prefix_blocks;  // shares of the prefix, blocks of rows
+  int prefix_wgs;                   // workgroups of a kv head for them here (none: the wide kernel has them)
   int own_parts, own_blocks, chunk; // chunks of a slot's rows (chunk rows each), blocks of rows
   float* part_o;    // [part][kv head][row][D], parts of the prefix first
   float* part_lse;  // [part][kv head][row], log2
@@ -81,14 +89,17 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
-// UNITS: groups of 32 rows that share the tiles.
-template <int UNITS>
-__global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixParams P) {
-  // one array per slot, so that alias analysis can tell a slot being loaded
-  // from the one being read; each wave has its own part of them
-  __shared__ __attribute__((aligned(16))) uint16_t K0[kWaves * kKSlot], K1[kWaves * kKSlot];
-  __shared__ __attribute__((aligned(16))) uint16_t V0[kWaves * kVSlot], V1[kWaves * kVSlot];
-  __shared__ int ids[kMaxIds];
+// Memory operations stay on their side of this: the counts of loads under way
+// that the kernel waits for go by the order it asks for them.
+__device__ __forceinline__ void in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+__global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParams P) {
+  // a part of each for every wave
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[kWaves * kKSlot];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[kWaves * kVSlot];
   __shared__ float wm[kWaves][32], wl[kWaves][32];
 
   const int tid = threadIdx.x;
@@ -100,13 +111,14 @@ __global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixPa
   const unsigned hkv = (unsigned)P.n_kv_heads;
   const int g = (int)(blockIdx.x % hkv);
   unsigned rest = blockIdx.x / hkv;
-  const unsigned n_prefix_wgs = (unsigned)P.prefix_parts * (unsigned)P.prefix_blocks;
+  const unsigned n_prefix_wgs = (unsigned)P.prefix_wgs;
   const bool own = rest >= n_prefix_wgs;
   int part, row0, row_end, key0, key_end, slot = 0, have = 0;
+  int page_id = -1;  // own: lane i has the number of the chunk's page i, -1 where the table names none of the pool
   if (!own) {
     const int rb = (int)(rest % (unsigned)P.prefix_blocks);
     part = (int)(rest / (unsigned)P.prefix_blocks);
-    row0 = rb * (32 * UNITS);
+    row0 = rb * 32;
     row_end = P.rows;
     const long long tiles = ((long long)P.n_prefix + kTile - 1) / kTile;
     key0 = (int)(tiles * part / P.prefix_parts) * kTile;
@@ -122,39 +134,37 @@ __global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixPa
     if (key0 >= have) return;  // every wave: nothing of this chunk is there, and the join knows it
     key_end = (int)std::min<long long>((long long)key0 + P.chunk, have);
     part = P.prefix_parts + c;
-    row0 = slot * P.slot_rows + rb * (32 * UNITS);
+    row0 = slot * P.slot_rows + rb * 32;
     row_end = (slot + 1) * P.slot_rows;
-    // the chunk's pages; an entry outside the pool has no rows
-    const int first = key0 >> P.pages.page_shift;
-    const int n_ids = ((key_end - 1) >> P.pages.page_shift) - first + 1;
-    for (int i = tid; i < n_ids; i += kThreads) {
-      const int p = P.pages.table[(size_t)slot * P.pages.max_pages + first + i];
-      ids[i] = p >= 0 && p < P.pages.n_pages ? p : -1;
+    const int first = key0 >> P.pages.page_shift;  // chunks start with a page
+    if (lane <= ((key_end - 1) >> P.pages.page_shift) - first) {
+      const int p = P.pages.table[(size_t)slot * P.pages.max_pages + first + lane];
+      page_id = p >= 0 && p < P.pages.n_pages ? p : -1;
     }
   }
+  // the page of a key of this chunk (the same key in every lane)
+  auto page_of = [&](int key) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readlane(page_id, (key - key0) >> P.pages.page_shift);
+  };
 
-  // queries of the rows, and how many keys of the tensor each row sees
-  bf16x8 qreg[UNITS][8];
-  int sees[UNITS];
-  int sees_least = 0x7fffffff;
-#pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    const int r = row0 + 32 * u + ql;
-    const bool in = r < row_end;
-    const int tok = r / P.group;
+  // query of the row, and how many keys of the tensor the row sees
+  bf16x8 qreg[8];
+  const int row = row0 + ql;
+  const bool in = row < row_end;
+  int sees = 0;
+  {
+    const int tok = row / P.group;
     const uint16_t* qp =
-        P.q + ((long long)tok * P.n_q_heads + g * P.group + (r - tok * P.group)) * kHeadDim + half * 8;
+        P.q + ((long long)tok * P.n_q_heads + g * P.group + (row - tok * P.group)) * kHeadDim + half * 8;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
-      qreg[u][ks] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(qp + ks * 16) : make_uint4(0, 0, 0, 0));
-    sees[u] = own ? max(have - P.n_new + (tok - slot * P.n_new) + 1, 0) : P.n_prefix;
-    if (in) sees_least = min(sees_least, sees[u]);
+      qreg[ks] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(qp + ks * 16) : make_uint4(0, 0, 0, 0));
+    sees = own ? max(have - P.n_new + (tok - slot * P.n_new) + 1, 0) : P.n_prefix;
   }
+  int sees_least = in ? sees : 0x7fffffff;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) sees_least = min(sees_least, __shfl_xor(sees_least, m));
   sees_least = __builtin_amdgcn_readfirstlane(sees_least);
-  const int units = min(UNITS, (row_end - row0 + 31) / 32);
-  __syncthreads();  // ids
 
   // A tile: eight loads of four rows of K, then eight of V; lane l of a load
   // fills 16 bytes at the wave's LDS address + 16 l.  LDS pieces are swizzled
@@ -164,42 +174,37 @@ __global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixPa
   const int lr = lane >> 4, lp = lane & 15;
   const int k_piece = 16 * (lp ^ lr), v_piece = 16 * (lp ^ (4 * lr));
   const char* zero = reinterpret_cast<const char*>(zero_row);
-  auto issue = [&](int k0, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
-    long long at[8];
+  const char* const kb = reinterpret_cast<const char*>(own ? P.kt : P.kp) + g * (kHeadDim * 2) + k_piece;
+  const char* const vb = reinterpret_cast<const char*>(own ? P.vt : P.vp) + g * (kHeadDim * 2) + v_piece;
+  uint16_t* const ks_ = Ks + wave * kKSlot;
+  uint16_t* const vs_ = Vs + wave * kVSlot;
+  // bytes to this lane's row of load j of the tile at k0, or -1
+  auto row_at = [&](int k0, int j) __attribute__((always_inline)) -> long long {
+    const int key = k0 + 4 * j + lr;
+    if (!own) return key >= key_end ? -1 : key * row_bytes;
+    const int id = page_of(min(k0 + 4 * j, key_end - 1));  // four rows share a page
+    const long long r = ((long long)id << P.pages.page_shift) + (key & ((1 << P.pages.page_shift) - 1));
+    return id < 0 || key >= key_end ? -1 : r * row_bytes;
+  };
+  auto issue_k = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int key = k0 + 4 * j + lr;
-      at[j] = -1;
-      if (key < key_end) {
-        long long r = key;
-        if (own) {
-          const int p = ids[(key >> P.pages.page_shift) - (key0 >> P.pages.page_shift)];
-          r = p < 0 ? -1 : ((long long)p << P.pages.page_shift) + (key & ((1 << P.pages.page_shift) - 1));
-        }
-        if (r >= 0) at[j] = r * row_bytes + g * (kHeadDim * 2);
-      }
+      const long long at = row_at(k0, j);
+      __builtin_amdgcn_global_load_lds((global_void*)(at >= 0 ? kb + at : zero + k_piece), (lds_void*)(ks_ + j * kKGroup), 16, 0, 0);
     }
-    const char* kb = reinterpret_cast<const char*>(own ? P.kt : P.kp);
-    const char* vb = reinterpret_cast<const char*>(own ? P.vt : P.vp);
+    in_order();
+  };
+  auto issue_v = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const char* from = (at[j] >= 0 ? kb + at[j] : zero) + k_piece;
-      __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)(ks_ + j * kKGroup), 16, 0, 0);
+      const long long at = row_at(k0, j);
+      __builtin_amdgcn_global_load_lds((global_void*)(at >= 0 ? vb + at : zero + v_piece), (lds_void*)(vs_ + 4 * j * kHeadDim), 16, 0, 0);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char* from = (at[j] >= 0 ? vb + at[j] : zero) + v_piece;
-      __builtin_amdgcn_global_load_lds((global_void*)from, (lds_void*)(vs_ + 4 * j * kHeadDim), 16, 0, 0);
-    }
+    in_order();
   };
   // Whether any of the pages is outside the pool: its keys are masked like
   // keys past the end.
-  int gaps = 0;
-  if (own) {
-    for (int i = lane; i <= ((key_end - 1) >> P.pages.page_shift) - (key0 >> P.pages.page_shift); i += 64)
-      gaps |= ids[i] < 0;
-    gaps = __any(gaps);
-  }
+  const bool gaps = own && __any(page_id < 0 && lane <= ((key_end - 1 - key0) >> P.pages.page_shift));
 
   // operand reads: A = K rows lane % 32, dims 16 ks + 8 half .. + 8; and
   // A = V^T, dims 32 dt + lane % 32, keys in the order in which the S^T
@@ -215,44 +220,47 @@ __global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixPa
       v_rd[dt] = (4 * half + sr) * kHeadDim + 32 * (dt ^ sr) + 16 * gd + 4 * (i & 3);
   }
 
-  f32x16 o[UNITS][4];
-  float m_run[UNITS], l_run[UNITS];
+  f32x16 o[4];
+  float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    m_run[u] = -INFINITY;
-    l_run[u] = 0.f;
+  for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[u][dt][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
 
-  auto tile = [&](int k0, const uint16_t* ks_, const uint16_t* vs_, auto&& wait_v) __attribute__((always_inline)) {
-    uint4 kf[8];
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) kf[ks] = *reinterpret_cast<const uint4*>(ks_ + k_rd[ks & 1] + 16 * ks);
-    bf16x8 pb[UNITS][2];
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      if (u >= units) break;
+  // Tile i of this wave starts at key0 + 32 (8 i + wave).  Loads return in
+  // order, K and V by turns, so whichever is needed next is there when at most
+  // eight are left.  A tile past the last is loaded too, as zeros (no memory
+  // traffic), so that these counts hold to the end.
+  const int n_all = (key_end - key0 + kTile - 1) / kTile;
+  const int n = n_all > wave ? (n_all - wave + kWaves - 1) / kWaves : 0;
+  auto start = [&](int i) __attribute__((always_inline)) { return i < n ? key0 + kTile * (kWaves * i + wave) : key_end; };
+  if (n > 0) {
+    // the queries' loads are done before the count of loads under way begins
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));
+    in_order();
+    issue_k(start(0));
+    issue_v(start(0));
+    for (int i = 0; i < n; ++i) {
+      const int k0 = start(i);
+      __builtin_amdgcn_s_waitcnt(wait_vm(8));  // K
+      in_order();
       f32x16 s = {};
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf[ks]), qreg[u][ks], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const uint4*>(ks_ + k_rd[ks & 1] + 16 * ks)), qreg[ks], s, 0, 0, 0);
+      in_order();
+      __builtin_amdgcn_s_waitcnt(kWaitLds);  // the slot has been read
+      issue_k(start(i + 1));
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= P.scale_log2;
       if (k0 + kTile > sees_least || k0 + kTile > key_end || gaps) {
-        // first key that is not seen, for each four keys of the lane (which
-        // share a page); as plain selects, no branch inside the unit
-        const int limit = min(sees[u], key_end);
+        // first key that is not seen, for each eight keys (which share a page)
+        const int limit = min(sees, key_end);
         int lim[4] = {limit, limit, limit, limit};
         if (gaps) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = min(k0 + 8 * j + half * 4, key_end - 1);
-            const int id = ids[(key >> P.pages.page_shift) - (key0 >> P.pages.page_shift)];
-            lim[j] = id < 0 ? key0 : limit;
-          }
+          for (int j = 0; j < 4; ++j) lim[j] = page_of(min(k0 + 8 * j, key_end - 1)) < 0 ? key0 : limit;
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r)
@@ -262,130 +270,89 @@ __global__ __launch_bounds__(kThreads, 1) void prefix_attn_kernel(const PrefixPa
 #pragma unroll
       for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      const float m_new = fmaxf(m_run[u], fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+      // The offset of a row's exponents follows the maximum only when that has
+      // left it by 2^8: weights up to 2^8 lose nothing, and O is seldom scaled.
+      const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      const float m_new = mx2 > m_run + 8.f ? mx2 : m_run;
       const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m_run[u] - m_use);
-      if (__any(m_new > m_run[u])) {
+      if (__any(m_new != m_run)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) o[u][dt][r] *= alpha;
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
       }
-      m_run[u] = m_new;
-      float sum = 0.f;
+      m_run = m_new;
       uint32_t w[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float p0 = __builtin_amdgcn_exp2f(s[2 * e] - m_use), p1 = __builtin_amdgcn_exp2f(s[2 * e + 1] - m_use);
-        sum += p0 + p1;
+        l_run += p0 + p1;
         w[e] = pack_bf16x2(p0, p1);
       }
-      l_run[u] = fmaf(l_run[u], alpha, sum);
-      pb[u][0] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
-      pb[u][1] = as_bf16x8(make_uint4(w[4], w[5], w[6], w[7]));
-    }
-    wait_v();
+      const bf16x8 pb[2] = {as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])), as_bf16x8(make_uint4(w[4], w[5], w[6], w[7]))};
+      __builtin_amdgcn_s_waitcnt(wait_vm(8));  // V
+      in_order();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int kk = i >> 2, dt = i & 3;
-      const uint16_t* b = vs_ + v_rd[dt] + kk * 16 * kHeadDim;
-      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b));
-      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b + 8 * kHeadDim));
-      const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
-      const bf16x8 vf = as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y));
-#pragma unroll
-      for (int u = 0; u < UNITS; ++u) {
-        if (u >= units) break;
-        o[u][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[u][kk], o[u][dt], 0, 0, 0);
+      for (int j = 0; j < 8; ++j) {
+        const int kk = j >> 2, dt = j & 3;
+        const uint16_t* b = vs_ + v_rd[dt] + kk * 16 * kHeadDim;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b + 8 * kHeadDim));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pb[kk], o[dt], 0, 0, 0);
       }
+      in_order();
+      __builtin_amdgcn_s_waitcnt(kWaitLds);
+      issue_v(start(i + 1));
     }
-  };
-
-  // Tile i of this wave starts at key0 + 32 (4 i + wave) and goes to slot i %
-  // 2.  Loads return in order: with the next tile's 16 under way, K is there
-  // when at most 24 are left, V when at most 16 are.
-  const int n_all = (key_end - key0 + kTile - 1) / kTile;
-  const int n = n_all > wave ? (n_all - wave + kWaves - 1) / kWaves : 0;
-  auto start = [&](int i) __attribute__((always_inline)) { return key0 + kTile * (kWaves * i + wave); };
-  uint16_t* const ks0 = K0 + wave * kKSlot;
-  uint16_t* const ks1 = K1 + wave * kKSlot;
-  uint16_t* const vs0 = V0 + wave * kVSlot;
-  uint16_t* const vs1 = V1 + wave * kVSlot;
-  auto step = [&](int i, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
-    const bool more = i + 1 < n;  // the same in every lane
-    if (more) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-    tile(start(i), ks_, vs_, [&]() __attribute__((always_inline)) {
-      if (more) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    });
-    if (i + 2 < n) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
-      issue(start(i + 2), ks_, vs_);
-    }
-  };
-  // the queries' loads are done before the count of loads under way begins
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (n > 0) issue(start(0), ks0, vs0);
-  if (n > 1) issue(start(1), ks1, vs1);
-  for (int i = 0; i < n; i += 2) {
-    step(i, ks0, vs0);
-    if (i + 1 < n) step(i + 1, ks1, vs1);
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));
   }
 
-  // join the waves, half the channels of a unit at a time (32 KB of LDS),
-  // in wave order
-  float4* const red = reinterpret_cast<float4*>(K0);
-  static_assert(sizeof(K0) >= kWaves * 8 * 64 * sizeof(float4), "the waves' sums of half the channels");
+  // join the waves, 32 channels at a time (32 KB of LDS), in wave order
+  float4* const red = reinterpret_cast<float4*>(Ks);
+  static_assert(sizeof(Ks) >= kWaves * 4 * 64 * sizeof(float4), "the waves' sums of a quarter of the channels");
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  if (half == 0) {
+    wm[wave][ql] = m_run;
+    wl[wave][ql] = l_tot;
+  }
+  __syncthreads();  // all waves are done with their slots
+  float m = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    if (u >= units) break;
-    const float l_tot = l_run[u] + __shfl_xor(l_run[u], 32);
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wm[w][ql]);
+  float l = 0.f, f[kWaves];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      __syncthreads();
-      if (half == 0 && hf == 0) {
-        wm[wave][ql] = m_run[u];
-        wl[wave][ql] = l_tot;
-      }
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = wm[w][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][ql] - m);
+    l = fmaf(f[w], wl[w][ql], l);
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const long long at = ((long long)part * P.n_kv_heads + g) * P.rows + row;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const f32x16& a = o[u][2 * hf + (e >> 2)];
-        const int rr = 4 * (e & 3);
-        red[(wave * 8 + e) * 64 + lane] = make_float4(a[rr], a[rr + 1], a[rr + 2], a[rr + 3]);
-      }
-      __syncthreads();
-      float m = -INFINITY;
+  for (int dt = 0; dt < 4; ++dt) {
+    if (dt) __syncthreads();
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wm[w][ql]);
-      float l = 0.f, f[kWaves];
+    for (int e = 0; e < 4; ++e)
+      red[(wave * 4 + e) * 64 + lane] = make_float4(o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]);
+    __syncthreads();
+    if (wave < 4) {  // piece `wave` of the four
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        f[w] = wm[w][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][ql] - m);
-        l = fmaf(f[w], wl[w][ql], l);
+        const float4 x = red[(w * 4 + wave) * 64 + lane];
+        a.x = fmaf(f[w], x.x, a.x);
+        a.y = fmaf(f[w], x.y, a.y);
+        a.z = fmaf(f[w], x.z, a.z);
+        a.w = fmaf(f[w], x.w, a.w);
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      const int r = row0 + 32 * u + ql;
-      const long long at = ((long long)part * P.n_kv_heads + g) * P.rows + r;
-#pragma unroll
-      for (int e2 = 0; e2 < 2; ++e2) {
-        const int e = 2 * wave + e2;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float4 x = red[(w * 8 + e) * 64 + lane];
-          a.x = fmaf(f[w], x.x, a.x);
-          a.y = fmaf(f[w], x.y, a.y);
-          a.z = fmaf(f[w], x.z, a.z);
-          a.w = fmaf(f[w], x.w, a.w);
-        }
-        if (r < row_end)
-          *reinterpret_cast<float4*>(P.part_o + at * kHeadDim + 64 * hf + 32 * (e >> 2) + 8 * (e & 3) + 4 * half) =
-              make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
-      }
-      if (hf == 0 && wave == 0 && half == 0 && r < row_end) P.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
+      if (in)
+        *reinterpret_cast<float4*>(P.part_o + at * kHeadDim + 32 * dt + 8 * wave + 4 * half) =
+            make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
     }
   }
+  if (wave == 0 && half == 0 && in) P.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
 }
 
 // Joins the parts of a row, one wave per row and head (two channels a lane),
@@ -429,25 +396,28 @@ long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 
 constexpr int kCus = 256;
 
-// How a call is cut.  Units of 32 rows that share a tile: as many as the rows
-// fill, up to two.  The prefix in as many shares as give every CU a
-// workgroup, each wave of it at least one tile; a slot's rows in chunks of
-// 512 (four tiles a wave) unless its table holds more than 32 of them.
+// How a call is cut.  Up to 32 rows of a kv head take the kernel here, more
+// the wide one, 256 rows a workgroup.  The prefix in as many shares as give
+// every CU a workgroup, of at least a tile for each wave here, of four 64-key
+// tiles there; a slot's rows in chunks of 512 (two tiles a wave), larger where
+// its table holds more than 32 of them, but of no more than 64 pages.
 struct Cut {
-  int units, prefix_parts, prefix_blocks, own_parts, own_blocks, chunk;
+  bool wide;
+  int prefix_parts, prefix_blocks, own_parts, own_blocks, chunk;
 };
 Cut cut(int64_t n_prefix, int64_t rows, int64_t slot_rows, int n_kv_heads, int page_rows, int max_pages) {
   Cut c;
-  c.units = rows <= 32 ? 1 : 2;
-  c.prefix_blocks = (int)div_up(rows, 32 * c.units);
-  const long long tiles = div_up(n_prefix, kTile);
-  c.prefix_parts = n_prefix == 0 || rows == 0 ? 0
-                                 : (int)std::max<long long>(1, std::min<long long>(div_up(kCus, (long long)n_kv_heads * c.prefix_blocks),
-                                                                                  div_up(tiles, kWaves)));
+  c.wide = rows > 32;
+  c.prefix_blocks = (int)div_up(rows, c.wide ? 256 : 32);
+  const long long most_parts = div_up(n_prefix, c.wide ? 4 * 64 : kTile * kWaves);
+  c.prefix_parts = n_prefix == 0 || rows == 0
+                       ? 0
+                       : (int)std::max<long long>(1, std::min(div_up(kCus, (long long)n_kv_heads * c.prefix_blocks), most_parts));
   const long long most = (long long)max_pages * page_rows;
   c.chunk = (int)std::min<long long>(std::max<long long>(512, div_up(most, 32 * 128) * 128), (long long)kMaxIds * page_rows);
+  c.chunk = std::max(c.chunk / page_rows, 1) * page_rows;  // whole pages
   c.own_parts = (int)div_up(most, c.chunk);
-  c.own_blocks = (int)div_up(slot_rows, 32 * c.units);
+  c.own_blocks = (int)div_up(slot_rows, 32);
   return c;
 }
 
@@ -497,11 +467,15 @@ hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t*
   P.part_lse = P.part_o + (size_t)(c.prefix_parts + c.own_parts) * n_kv_heads * P.rows * kHeadDim;
   P.out = out;
   P.lse = lse;
-  const long long wgs = ((long long)c.prefix_parts * c.prefix_blocks + (long long)c.own_parts * c.own_blocks * P.n_slots) * n_kv_heads;
+  if (c.wide && c.prefix_parts > 0) {
+    const hipError_t e = launch_prefix_rows(q, P.rows, n_q_heads, n_kv_heads, kp, vp, n_prefix, c.prefix_parts, scale,
+                                            P.part_o, P.part_lse, s);
+    if (e != hipSuccess) return e;
+  }
+  P.prefix_wgs = c.wide ? 0 : c.prefix_parts * c.prefix_blocks;
+  const long long wgs = (P.prefix_wgs + (long long)c.own_parts * c.own_blocks * P.n_slots) * n_kv_heads;
   if (wgs > 0) {
-    const dim3 grid((unsigned)wgs), block(kThreads);
-    if (c.units == 1) hipLaunchKernelGGL(prefix_attn_kernel<1>, grid, block, 0, s, P);
-    else hipLaunchKernelGGL(prefix_attn_kernel<2>, grid, block, 0, s, P);
+    hipLaunchKernelGGL(prefix_attn_kernel, dim3((unsigned)wgs), dim3(kThreads), 0, s, P);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
