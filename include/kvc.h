@@ -620,7 +620,7 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
  * the product with V.  ws: kvc_shared_prefix_workspace bytes (a part's float32
  * results for each part of the keys, so it grows with max_pages), 16-byte
  * aligned.  The same call gives the same bits.  n_slots x n_new x Hq is at
- * most 2^25.
+ * most 2^23.
  */
 #define KVC_SHARED_MAX_NEW 4096
 kvc_status kvc_shared_prefix_workspace(const kvc_pages* P, int64_t n_prefix, int32_t n_new,

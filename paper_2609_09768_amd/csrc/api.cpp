@@ -1477,8 +1477,8 @@ static kvc_status check_shared(const char* W, const kvc_pages* P, int64_t n_pref
     return fail(KVC_ERR_INVALID_ARG, "%s: n_prefix=%lld out of range", W, (long long)n_prefix);
   if (n_new < 1 || n_new > KVC_SHARED_MAX_NEW)
     return fail(KVC_ERR_INVALID_ARG, "%s: n_new=%d must be in [1, %d]", W, n_new, KVC_SHARED_MAX_NEW);
-  // one launch: fewer than 2^32 work-items, 64 for each query and head
-  if ((int64_t)P->n_slots * n_new * n_q_heads > (int64_t(1) << 25) ||
+  // one launch: fewer than 2^32 work-items, 256 for each query and head
+  if ((int64_t)P->n_slots * n_new * n_q_heads > (int64_t(1) << 23) ||
       kvc::prefix_attention_workgroups(n_prefix, P->n_slots, n_new, n_q_heads, n_kv_heads, P->page_rows, P->max_pages) >
           (int64_t(1) << 22))
     return fail(KVC_ERR_INVALID_ARG, "%s: too many slots, queries and heads for one launch", W);

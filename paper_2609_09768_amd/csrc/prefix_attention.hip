@@ -15,8 +15,9 @@
 //
 // Up to 32 rows of a kv head are bound by the bytes of K and V: 512 per key
 // and kv head against 4 x 128 FLOP per row.  So the kernel here is built
-// around loads in flight.  A workgroup has eight waves, two per SIMD; each
-// takes every eighth 32-key tile of the part by itself, with a K slot and a V
+// around loads in flight.  A workgroup has four waves, and two fit a CU, so that
+// one's first loads and joins lie beside the other's tiles; each wave takes
+// every fourth 32-key tile of the part by itself, with a K slot and a V
 // slot of its own in LDS that loads fill without registers: the next K tile is
 // asked for when the scores are done, the next V tile when the product is, so
 // 64 to 128 KB per CU are under way, and no barrier is met until the waves join
@@ -46,8 +47,9 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 typedef __attribute__((address_space(1))) const void global_void;
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+static_assert(kWaves == 4, "the join gives each wave a quarter of 32 channels");
 constexpr int kTile = 32;                       // keys of a tile
 constexpr int kKGroup = 4 * kHeadDim + 32;      // bf16 per four K rows in LDS (1088 B, spreads the banks)
 constexpr int kKSlot = (kTile / 4) * kKGroup;   // of one wave
@@ -96,7 +98,7 @@ __device__ __forceinline__ void in_order() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-__global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParams P) {
+__global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixParams P) {
   // a part of each for every wave
   __shared__ __attribute__((aligned(16))) uint16_t Ks[kWaves * kKSlot];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[kWaves * kVSlot];
@@ -178,30 +180,36 @@ __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParam
   const char* const vb = reinterpret_cast<const char*>(own ? P.vt : P.vp) + g * (kHeadDim * 2) + v_piece;
   uint16_t* const ks_ = Ks + wave * kKSlot;
   uint16_t* const vs_ = Vs + wave * kVSlot;
-  // bytes to this lane's row of load j of the tile at k0, or -1
-  auto row_at = [&](int k0, int j) __attribute__((always_inline)) -> long long {
-    const int key = k0 + 4 * j + lr;
-    if (!own) return key >= key_end ? -1 : key * row_bytes;
-    const int id = page_of(min(k0 + 4 * j, key_end - 1));  // four rows share a page
-    const long long r = ((long long)id << P.pages.page_shift) + (key & ((1 << P.pages.page_shift) - 1));
-    return id < 0 || key >= key_end ? -1 : r * row_bytes;
-  };
-  auto issue_k = [&](int k0) __attribute__((always_inline)) {
+  // Loads of a K or V tile (base: kb or vb; row r goes to to + r's place).  A
+  // row that is not there is loaded as zeros.
+  auto issue = [&](int k0, const char* base, int piece, uint16_t* to, int stride) __attribute__((always_inline)) {
+    const char* from[8];
+    if (!own && k0 + kTile <= key_end) {
+      from[0] = base + (long long)(k0 + lr) * row_bytes;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const long long at = row_at(k0, j);
-      __builtin_amdgcn_global_load_lds((global_void*)(at >= 0 ? kb + at : zero + k_piece), (lds_void*)(ks_ + j * kKGroup), 16, 0, 0);
+      for (int j = 1; j < 8; ++j) from[j] = from[j - 1] + 4 * row_bytes;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = k0 + 4 * j + lr;
+        long long r = key;
+        int id = 0;
+        if (own) {
+          id = page_of(min(k0 + 4 * j, key_end - 1));  // four rows share a page
+          r = ((long long)id << P.pages.page_shift) + (key & ((1 << P.pages.page_shift) - 1));
+        }
+        from[j] = id < 0 || key >= key_end ? zero + piece : base + r * row_bytes;
+      }
     }
+    // (one place for the loads: the compiler's wait counting goes by it)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      __builtin_amdgcn_global_load_lds((global_void*)from[j], (lds_void*)(to + j * stride), 16, 0, 0);
     in_order();
   };
-  auto issue_v = [&](int k0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const long long at = row_at(k0, j);
-      __builtin_amdgcn_global_load_lds((global_void*)(at >= 0 ? vb + at : zero + v_piece), (lds_void*)(vs_ + 4 * j * kHeadDim), 16, 0, 0);
-    }
-    in_order();
-  };
+  auto issue_k = [&](int k0) __attribute__((always_inline)) { issue(k0, kb, k_piece, ks_, kKGroup); };
+  auto issue_v = [&](int k0) __attribute__((always_inline)) { issue(k0, vb, v_piece, vs_, 4 * kHeadDim); };
+
   // Whether any of the pages is outside the pool: its keys are masked like
   // keys past the end.
   const bool gaps = own && __any(page_id < 0 && lane <= ((key_end - 1 - key0) >> P.pages.page_shift));
@@ -227,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParam
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
 
-  // Tile i of this wave starts at key0 + 32 (8 i + wave).  Loads return in
+  // Tile i of this wave starts at key0 + 32 (4 i + wave).  Loads return in
   // order, K and V by turns, so whichever is needed next is there when at most
   // eight are left.  A tile past the last is loaded too, as zeros (no memory
   // traffic), so that these counts hold to the end.
@@ -310,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParam
     __builtin_amdgcn_s_waitcnt(wait_vm(0));
   }
 
-  // join the waves, 32 channels at a time (32 KB of LDS), in wave order
+  // join the waves, 32 channels at a time (16 KB of LDS), in wave order
   float4* const red = reinterpret_cast<float4*>(Ks);
   static_assert(sizeof(Ks) >= kWaves * 4 * 64 * sizeof(float4), "the waves' sums of a quarter of the channels");
   const float l_tot = l_run + __shfl_xor(l_run, 32);
@@ -337,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParam
     for (int e = 0; e < 4; ++e)
       red[(wave * 4 + e) * 64 + lane] = make_float4(o[dt][4 * e], o[dt][4 * e + 1], o[dt][4 * e + 2], o[dt][4 * e + 3]);
     __syncthreads();
-    if (wave < 4) {  // piece `wave` of the four
+    {  // piece `wave` of the four
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
@@ -355,14 +363,17 @@ __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(const PrefixParam
   if (wave == 0 && half == 0 && in) P.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
 }
 
-// Joins the parts of a row, one wave per row and head (two channels a lane),
-// in the order of the parts: weights 2^(lse - max).
-constexpr int kJoinThreads = 256;
-__global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixParams P) {
+// Joins the parts of a row and head with the weights 2^(lse - max), one
+// workgroup each: a lane has the weight of one of 64 parts, each wave adds
+// every fourth part (two channels a lane, up to eight parts' loads under way),
+// and the waves' sums are added in order.  Bound by the parts' 516 bytes a row,
+// and by two rounds of loads.
+constexpr int kJoinWaves = 4;
+__global__ __launch_bounds__(64 * kJoinWaves) void prefix_join_kernel(const PrefixParams P) {
+  __shared__ float2 sums[kJoinWaves][64];
   const int lane = threadIdx.x & 63;
-  const long long i = (long long)blockIdx.x * (kJoinThreads / 64) + (threadIdx.x >> 6);
-  if (i >= (long long)P.rows * P.n_kv_heads) return;
-  const int g = (int)(i / P.rows), r = (int)(i - (long long)g * P.rows);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = (int)(blockIdx.x / (unsigned)P.rows), r = (int)(blockIdx.x - (unsigned)g * (unsigned)P.rows);
   const int tok = r / P.group, h = g * P.group + (r - tok * P.group), slot = tok / P.n_new;
   const int have = min(max(P.pages.len[slot], 0), P.pages.max_pages << P.pages.page_shift);
   const int t = have - P.n_new + (tok - slot * P.n_new);  // its place among the slot's rows
@@ -371,20 +382,42 @@ __global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixP
   const long long stride = (long long)P.n_kv_heads * P.rows;
   const float* lp = P.part_lse + (long long)g * P.rows + r;
   const float* op = P.part_o + ((long long)g * P.rows + r) * kHeadDim + 2 * lane;
-  float m = -INFINITY;
-  for (int p = lane; p < parts; p += 64) m = fmaxf(m, lp[p * stride]);
+  float l_first = lane < parts ? lp[lane * stride] : -INFINITY;
+  float m = l_first;
+  for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, lp[p * stride]);
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
   float a = 0.f, b = 0.f, sum = 0.f;
-  if (m != -INFINITY) {
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) {
-      const float w = __builtin_amdgcn_exp2f(lp[p * stride] - m);
-      const float2 x = *reinterpret_cast<const float2*>(op + p * stride * kHeadDim);
-      a = fmaf(w, x.x, a);
-      b = fmaf(w, x.y, b);
-      sum += w;
+  for (int p0 = 0; p0 < parts && m != -INFINITY; p0 += 64) {
+    const float l = p0 == 0 ? l_first : p0 + lane < parts ? lp[(p0 + lane) * stride] : -INFINITY;
+    const float w = __builtin_amdgcn_exp2f(l - m);  // 0 for a part without keys
+    sum += w;
+    const int n = min(parts - p0, 64);
+    const float* q = op + (long long)p0 * stride * kHeadDim;
+#pragma unroll 1
+    for (int p = wave; p < n; p += 8 * kJoinWaves) {
+      float2 x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        x[e] = p + e * kJoinWaves < n ? *reinterpret_cast<const float2*>(q + (p + e * kJoinWaves) * stride * kHeadDim)
+                                      : make_float2(0.f, 0.f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float we = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), min(p + e * kJoinWaves, 63)));
+        a = fmaf(we, x[e].x, a);
+        b = fmaf(we, x[e].y, b);
+      }
     }
+  }
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+  sums[wave][lane] = make_float2(a, b);
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w) {
+    a += sums[w][lane].x;
+    b += sums[w][lane].y;
   }
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
   const long long at = (long long)tok * P.n_q_heads + h;
@@ -395,11 +428,12 @@ __global__ __launch_bounds__(kJoinThreads) void prefix_join_kernel(const PrefixP
 long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 
 constexpr int kCus = 256;
+constexpr int kPerCu = 2;  // workgroups of the kernel here that a CU holds (67 KB of LDS each)
 
 // How a call is cut.  Up to 32 rows of a kv head take the kernel here, more
-// the wide one, 256 rows a workgroup.  The prefix in as many shares as give
-// every CU a workgroup, of at least a tile for each wave here, of four 64-key
-// tiles there; a slot's rows in chunks of 512 (two tiles a wave), larger where
+// the wide one, 256 rows a workgroup.  The prefix in as many shares as fill
+// the CUs with workgroups, of at least a tile for each wave here, of four 64-key
+// tiles there; a slot's rows in chunks of 512 (four tiles a wave), larger where
 // its table holds more than 32 of them, but of no more than 64 pages.
 struct Cut {
   bool wide;
@@ -412,7 +446,7 @@ Cut cut(int64_t n_prefix, int64_t rows, int64_t slot_rows, int n_kv_heads, int p
   const long long most_parts = div_up(n_prefix, c.wide ? 4 * 64 : kTile * kWaves);
   c.prefix_parts = n_prefix == 0 || rows == 0
                        ? 0
-                       : (int)std::max<long long>(1, std::min(div_up(kCus, (long long)n_kv_heads * c.prefix_blocks), most_parts));
+                       : (int)std::max<long long>(1, std::min(div_up(c.wide ? kCus : kCus * kPerCu, (long long)n_kv_heads * c.prefix_blocks), most_parts));
   const long long most = (long long)max_pages * page_rows;
   c.chunk = (int)std::min<long long>(std::max<long long>(512, div_up(most, 32 * 128) * 128), (long long)kMaxIds * page_rows);
   c.chunk = std::max(c.chunk / page_rows, 1) * page_rows;  // whole pages
@@ -479,8 +513,7 @@ hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t*
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const long long waves = (long long)P.rows * n_kv_heads;
-  hipLaunchKernelGGL(prefix_join_kernel, dim3((unsigned)div_up(waves, kJoinThreads / 64)), dim3(kJoinThreads), 0, s, P);
+  hipLaunchKernelGGL(prefix_join_kernel, dim3((unsigned)P.rows * (unsigned)n_kv_heads), dim3(64 * kJoinWaves), 0, s, P);
   return hipGetLastError();
 }
 
