@@ -141,14 +141,22 @@ __device__ __forceinline__ void rotate8_f32(const uint4& a, const uint4& b, cons
   ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
 }
 
+// Sum over the eight lanes that share a head, in every one of them: the other
+// lane of a pair, the other pair of four, the other four mirrored.
+__device__ __forceinline__ float sum8(float x) {
+  x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0xB1, 0xF, 0xF, true));   // quad_perm 1 0 3 2
+  x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x4E, 0xF, 0xF, true));   // quad_perm 2 3 0 1
+  x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x141, 0xF, 0xF, true));  // row_half_mirror
+  return x;
+}
+
 // The RMS norm of a head of 128 in the registers of the eight lanes that hold
-// it (a: elements 8 jg .., b: 64 + 8 jg ..), in float32, then the rotation of
-// the unrounded values: x' = x / sqrt(mean x^2 + eps) * gamma, rounded once
-// after the rotation.  g: the head's 128 weights.
-__device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, const uint16_t* g, int jg, float eps,
-                                             const float* c, const float* s, uint4& oa, uint4& ob) {
-  const uint4 ga = *reinterpret_cast<const uint4*>(g + 8 * jg);
-  const uint4 gb = *reinterpret_cast<const uint4*>(g + kHalf + 8 * jg);
+// it (a: elements 8 jg .., b: 64 + 8 jg .., with the weights ga, gb), in
+// float32, then the rotation of the unrounded values: x' = x / sqrt(mean x^2 +
+// eps) * gamma, rounded once after the rotation.  The hardware's reciprocal
+// root is within one float32 unit.
+__device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, const uint4& ga, const uint4& gb,
+                                             float eps, const float* c, const float* s, uint4& oa, uint4& ob) {
   float ss = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -156,9 +164,7 @@ __device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, con
     ss = fmaf(x, x, ss);
     ss = fmaf(y, y, ss);
   }
-#pragma unroll
-  for (int m = 1; m <= 4; m <<= 1) ss += __shfl_xor(ss, m, 64);
-  const float inv = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + eps);
+  const float inv = __builtin_amdgcn_rsqf(sum8(ss) * (1.0f / kHeadDim) + eps);
   uint32_t ra[4], rb[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -178,9 +184,23 @@ __device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, con
   ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
 }
 
+__device__ __forceinline__ uint4 pick(bool first, const uint4& a, const uint4& b) {
+  return make_uint4(first ? a.x : b.x, first ? a.y : b.y, first ? a.z : b.z, first ? a.w : b.w);
+}
+
 template <bool NORM>
 __global__ __launch_bounds__(64 * kRopeWaves) void qkv_rope_kernel(const QkvRopeArgs A) {
   const int lane = threadIdx.x & 63;
+  // the weights of the lane's elements (NULL where no head uses them)
+  uint4 gq[2] = {}, gk[2] = {};
+  if constexpr (NORM) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = i * kHalf + 8 * (lane & 7);
+      if (A.gamma_q) gq[i] = *reinterpret_cast<const uint4*>(A.gamma_q + at);
+      if (A.gamma_k) gk[i] = *reinterpret_cast<const uint4*>(A.gamma_k + at);
+    }
+  }
   // one row per wave at a time; the row index is the same in every lane, so
   // the shuffles below always have the whole wave
   for (int64_t i = (int64_t)blockIdx.x * kRopeWaves + (threadIdx.x >> 6); i < A.n;
@@ -235,7 +255,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qkv_rope_kernel(const QkvRope
         uint16_t* dst = h < A.n_q ? A.q + (i * A.n_q + h) * kHeadDim
                                   : A.k + (i * A.n_k + (h - A.n_q)) * kHeadDim;
         uint4 oa, ob;
-        if constexpr (NORM) norm_rotate8(a[t], b[t], h < A.n_q ? A.gamma_q : A.gamma_k, jg, A.eps, c, s, oa, ob);
+        if constexpr (NORM)
+          norm_rotate8(a[t], b[t], pick(h < A.n_q, gq[0], gk[0]), pick(h < A.n_q, gq[1], gk[1]), A.eps, c, s, oa, ob);
         else rotate8_f32(a[t], b[t], c, s, oa, ob);
         *reinterpret_cast<uint4*>(dst + 8 * jg) = oa;
         *reinterpret_cast<uint4*>(dst + kHalf + 8 * jg) = ob;

@@ -13,7 +13,7 @@
 // (sequence, token, query head of the group) of a kv head, and every
 // sequence's own rows into chunks.
 //
-// Up to 32 rows of a kv head are bound by the bytes of K and V: 512 per key
+// Up to 64 rows of a kv head are bound by the bytes of K and V: 512 per key
 // and kv head against 4 x 128 FLOP per row.  So the kernel here is built
 // around loads in flight.  A workgroup has four waves, and two fit a CU, so that
 // one's first loads and joins lie beside the other's tiles; each wave takes
@@ -430,25 +430,30 @@ long long div_up(long long a, long long b) { return (a + b - 1) / b; }
 constexpr int kCus = 256;
 constexpr int kPerCu = 2;  // workgroups of the kernel here that a CU holds (67 KB of LDS each)
 
-// How a call is cut.  Up to 32 rows of a kv head take the kernel here, more
-// the wide one, 256 rows a workgroup.  The prefix in as many shares as fill
-// the CUs with workgroups, of at least a tile for each wave here, of four 64-key
-// tiles there; a slot's rows in chunks of 512 (four tiles a wave), larger where
+// How a call is cut.  Up to 64 rows of a kv head take the kernel here (a
+// second block of 32 finds the tiles in L2: 64 rows over 32,256 keys of 8
+// heads 47 us, 50 with the wide kernel, of whose eight waves two have work),
+// more the wide one, 256 rows a workgroup.  The prefix in as many shares as
+// fill the CUs with workgroups, of at least a tile for each wave here, of four
+// 64-key tiles there.  A slot's rows in chunks of 256 (two tiles a wave), 512
+// where slots and heads alone give every CU a workgroup (16 slots of 8 heads
+// and 300 rows 47 us, 50 with 512; 64 slots 170 us, 168 with 512), larger where
 // its table holds more than 32 of them, but of no more than 64 pages.
 struct Cut {
   bool wide;
   int prefix_parts, prefix_blocks, own_parts, own_blocks, chunk;
 };
-Cut cut(int64_t n_prefix, int64_t rows, int64_t slot_rows, int n_kv_heads, int page_rows, int max_pages) {
+Cut cut(int64_t n_prefix, int n_slots, int64_t rows, int64_t slot_rows, int n_kv_heads, int page_rows, int max_pages) {
   Cut c;
-  c.wide = rows > 32;
+  c.wide = rows > 64;
   c.prefix_blocks = (int)div_up(rows, c.wide ? 256 : 32);
   const long long most_parts = div_up(n_prefix, c.wide ? 4 * 64 : kTile * kWaves);
   c.prefix_parts = n_prefix == 0 || rows == 0
                        ? 0
                        : (int)std::max<long long>(1, std::min(div_up(c.wide ? kCus : kCus * kPerCu, (long long)n_kv_heads * c.prefix_blocks), most_parts));
   const long long most = (long long)max_pages * page_rows;
-  c.chunk = (int)std::min<long long>(std::max<long long>(512, div_up(most, 32 * 128) * 128), (long long)kMaxIds * page_rows);
+  const long long least = (long long)n_slots * n_kv_heads > kCus ? 512 : 256;
+  c.chunk = (int)std::min<long long>(std::max<long long>(least, div_up(most, 32 * 128) * 128), (long long)kMaxIds * page_rows);
   c.chunk = std::max(c.chunk / page_rows, 1) * page_rows;  // whole pages
   c.own_parts = (int)div_up(most, c.chunk);
   c.own_blocks = (int)div_up(slot_rows, 32);
@@ -460,14 +465,14 @@ Cut cut(int64_t n_prefix, int64_t rows, int64_t slot_rows, int n_kv_heads, int p
 size_t prefix_attention_ws_bytes(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
                                  int page_rows, int max_pages) {
   const int64_t slot_rows = (int64_t)n_new * (n_q_heads / n_kv_heads), rows = slot_rows * n_slots;
-  const Cut c = cut(n_prefix, rows, slot_rows, n_kv_heads, page_rows, max_pages);
+  const Cut c = cut(n_prefix, n_slots, rows, slot_rows, n_kv_heads, page_rows, max_pages);
   return align256(size_t(c.prefix_parts + c.own_parts) * size_t(n_kv_heads) * size_t(rows) * (kHeadDim + 1) * sizeof(float));
 }
 
 int64_t prefix_attention_workgroups(int64_t n_prefix, int n_slots, int n_new, int n_q_heads, int n_kv_heads,
                                     int page_rows, int max_pages) {
   const int64_t slot_rows = (int64_t)n_new * (n_q_heads / n_kv_heads), rows = slot_rows * n_slots;
-  const Cut c = cut(n_prefix, rows, slot_rows, n_kv_heads, page_rows, max_pages);
+  const Cut c = cut(n_prefix, n_slots, rows, slot_rows, n_kv_heads, page_rows, max_pages);
   return ((int64_t)c.prefix_parts * c.prefix_blocks + (int64_t)c.own_parts * c.own_blocks * n_slots) * n_kv_heads;
 }
 
@@ -491,7 +496,7 @@ hipError_t launch_prefix_attention(const uint16_t* q, int n_new, const uint16_t*
   P.vt = vt;
   P.pages = pages;
   P.scale_log2 = scale * 1.4426950408889634f;
-  const Cut c = cut(n_prefix, P.rows, P.slot_rows, n_kv_heads, 1 << pages.page_shift, pages.max_pages);
+  const Cut c = cut(n_prefix, P.n_slots, P.rows, P.slot_rows, n_kv_heads, 1 << pages.page_shift, pages.max_pages);
   P.prefix_parts = c.prefix_parts;
   P.prefix_blocks = c.prefix_blocks;
   P.own_parts = c.own_parts;
