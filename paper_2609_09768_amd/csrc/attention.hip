@@ -614,22 +614,54 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32);
-  if (!in_range) return;
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
   if constexpr (PACKED) {
-    if (item.part >= 0) {
-      // a unit's place is full size: 16 x [half][query] pieces of 4 channels
-      const long long at = (((long long)item.part * P.n_kv_heads + g) * kWaves + wave) * 32;
-      float4* po = reinterpret_cast<float4*>(P.part_o + at * kHeadDim) + half * 32 + ql;
+    if (item.part < 0) {
+      // Whole rows through LDS (272 bytes apart, in what were the K slots),
+      // four of them per store: short sequences spend much of their time here,
+      // and 8-byte pieces of 32 rows took 67 of 239 us for 32,000 rows of
+      // documents.
+      static_assert(2 * 32 * 136 <= kKSlot, "two waves' rows in a K slot");
+      const float inv_l = l_tot > 0.f ? 1.f / l_tot : 0.f;
+      __builtin_amdgcn_s_waitcnt(0 | 7 << 4);  // loads into the slots and reads of them are done
+      __builtin_amdgcn_s_barrier();
+      uint16_t* const rows = (wave < 2 ? K0 : wave < 4 ? K1 : wave < 6 ? K2 : K3) + (wave & 1) * (32 * 136);
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr)
-          po[(dt * 4 + rr) * 64] =
-              make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
-      if (half == 0) P.part_lse[at + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+          *reinterpret_cast<uint2*>(rows + ql * 136 + dt * 32 + rr * 8 + half * 4) =
+              make_uint2(pack_bf16x2(o[dt][rr * 4 + 0] * inv_l, o[dt][rr * 4 + 1] * inv_l),
+                         pack_bf16x2(o[dt][rr * 4 + 2] * inv_l, o[dt][rr * 4 + 3] * inv_l));
+      __builtin_amdgcn_wave_barrier();
+      uint4 line[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        line[j] = *reinterpret_cast<const uint4*>(rows + (4 * j + (lane >> 4)) * 136 + 8 * (lane & 15));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const long long r = 32ll * sub + 4 * j + (lane >> 4);
+        if (r < n_sel)
+          *reinterpret_cast<uint4*>(P.out + ((row0 + r) * P.n_q_heads + h) * (long long)kHeadDim + 8 * (lane & 15)) = line[j];
+      }
+      if (P.lse && half == 0 && in_range)
+        P.lse[(row0 + qi) * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
       return;
     }
+  }
+  if (!in_range) return;
+  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  if constexpr (PACKED) {
+    // a unit's place is full size: 16 x [half][query] pieces of 4 channels
+    const long long at = (((long long)item.part * P.n_kv_heads + g) * kWaves + wave) * 32;
+    float4* po = reinterpret_cast<float4*>(P.part_o + at * kHeadDim) + half * 32 + ql;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr)
+        po[(dt * 4 + rr) * 64] =
+            make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
+    if (half == 0) P.part_lse[at + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+    return;
   }
   if constexpr (PREFIX) {
     const long long at = ((long long)split * P.n_kv_heads + g) * n_sel + qi;
@@ -643,7 +675,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     if (half == 0) P.part_lse[at] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
     return;
   }
-  if (!PACKED && P.n_split > 1) {
+  if (P.n_split > 1) {
     const long long pair0 = ((long long)split * P.n_kv_heads + g) * P.n_sel * P.group + first_pair(P, unit);
     const int c = (int)std::min<long long>(32, P.n_sel - 32ll * sub);
     float4* po = reinterpret_cast<float4*>(P.part_o + pair0 * kHeadDim) + half * c + ql;
@@ -656,7 +688,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     if (half == 0) P.part_lse[pair0 + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
     return;
   }
-  uint16_t* op = P.out + ((row0 + qi) * P.n_q_heads + h) * (long long)kHeadDim + half * 4;
+  uint16_t* op = P.out + (qi * P.n_q_heads + h) * (long long)kHeadDim + half * 4;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -666,7 +698,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       *reinterpret_cast<uint2*>(op + dt * 32 + rr * 8) = make_uint2(w0, w1);
     }
   if (P.lse && half == 0)
-    P.lse[(row0 + qi) * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+    P.lse[qi * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
 }
 
 // Merge of the split partials of one unit's queries, one wave per 32 channels
