@@ -1260,15 +1260,20 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
 namespace {
 
 // ---- packed sequences -------------------------------------------------------------
-constexpr int kPackUnits = 8;   // units of 32 queries and a head in a workgroup
-constexpr int kPackTile = 64;   // keys of a tile
+constexpr int kPackTile = 64;  // keys of a tile
 constexpr int kCus = 256;
 
-// A block of a sequence: units 8 block .. 8 block + 7 of ceil(len / 32) groups
-// of queries times `group` heads, and the key tiles up to its last query.
-int64_t pack_blocks(int64_t len, int group) { return ((len + 31) / 32 * group + kPackUnits - 1) / kPackUnits; }
+// A block of a sequence: as many of its ceil(len / 32) groups of queries times
+// `group` heads as a workgroup has units, and the key tiles up to the last
+// query.
+int pack_units(int64_t len) { return len <= kvc::kPackShort ? kvc::kPackShortUnits : kvc::kPackUnits; }
+int64_t pack_blocks(int64_t len, int group) {
+  const int units = pack_units(len);
+  return ((len + 31) / 32 * group + units - 1) / units;
+}
 int pack_tiles(int64_t len, int group, int64_t block) {
-  const int64_t last = std::min<int64_t>(32 * ((kPackUnits * block + kPackUnits - 1) / group + 1), len) - 1;
+  const int units = pack_units(len);
+  const int64_t last = std::min<int64_t>(32 * ((units * block + units - 1) / group + 1), len) - 1;
   return (int)(last / kPackTile) + 1;
 }
 // Parts a block's tiles are cut into.  Blocks run longest first, so the batch
@@ -1283,7 +1288,7 @@ int pack_parts(int tiles, int64_t share) {
 }
 
 struct PackInfo {
-  int64_t n_rows = 0, n_items = 0, n_joins = 0, n_parts = 0;
+  int64_t n_rows = 0, n_items = 0, n_short = 0, n_joins = 0, n_parts = 0;  // items of long and of short sequences
   int64_t share = 0;  // about a CU's share of the key tiles
 };
 
@@ -1305,18 +1310,19 @@ kvc_status check_pack(const char* W, const kvc_pack* P, PackInfo* info) {
     if (i.n_rows > kMaxRows) return fail(KVC_ERR_INVALID_ARG, "%s: too many rows", W);
     const int64_t n = pack_blocks(len, group);
     const int tiles = pack_tiles(len, group, n - 1);
-    i.n_items += n;
-    twice += n * (pack_tiles(len, group, 0) + tiles);
-    longest = std::max(longest, tiles);
+    const bool is_short = len <= kvc::kPackShort;
+    (is_short ? i.n_short : i.n_items) += n;
+    twice += n * (pack_tiles(len, group, 0) + tiles) / (is_short ? 2 : 1);
+    if (!is_short) longest = std::max(longest, tiles);
   }
   // one launch: fewer than 2^32 work-items, cut blocks included (those are
   // cut only where there are few, see pack_parts)
-  if (i.n_items * P->n_kv_heads > (int64_t(1) << 22))
+  if ((i.n_items + i.n_short) * P->n_kv_heads > (int64_t(1) << 22))
     return fail(KVC_ERR_INVALID_ARG, "%s: too many queries and heads for one launch", W);
   i.share = (twice * P->n_kv_heads + 2 * kCus - 1) / (2 * kCus);
   if (pack_parts(longest, i.share) > 1)
     for (int32_t s = 0; s < P->n_seqs; ++s)
-      for (int64_t b = 0, n = pack_blocks(P->seq_len[s], group); b < n; ++b) {
+      for (int64_t b = 0, n = P->seq_len[s] > kvc::kPackShort ? pack_blocks(P->seq_len[s], group) : 0; b < n; ++b) {
         const int parts = pack_parts(pack_tiles(P->seq_len[s], group, b), i.share);
         if (parts == 1) continue;
         i.n_items += parts - 1;
@@ -1338,7 +1344,7 @@ uint64_t pack_id(const kvc_pack* P) {
 }
 
 size_t pack_bytes(const PackInfo& i) {
-  return kvc::pack_joins_offset(i.n_items) + kvc::align256(sizeof(kvc::PackJoin) * (size_t)i.n_joins);
+  return kvc::pack_joins_offset(i.n_items + i.n_short) + kvc::align256(sizeof(kvc::PackJoin) * (size_t)i.n_joins);
 }
 
 // The plan's image: work items, those with the most tiles first.
@@ -1348,16 +1354,22 @@ void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
   std::memset(&hdr, 0, sizeof(hdr));
   hdr.id = pack_id(P);
   hdr.n_items = (int32_t)info.n_items;
+  hdr.n_short = (int32_t)info.n_short;
   hdr.n_joins = (int32_t)info.n_joins;
   hdr.n_parts = (int32_t)info.n_parts;
   std::memcpy(img, &hdr, sizeof(hdr));
   kvc::PackItem* items = reinterpret_cast<kvc::PackItem*>(img + kvc::pack_items_offset());
-  kvc::PackJoin* joins = reinterpret_cast<kvc::PackJoin*>(img + kvc::pack_joins_offset(info.n_items));
-  int64_t row0 = 0, n = 0, nj = 0, np = 0;
+  kvc::PackJoin* joins = reinterpret_cast<kvc::PackJoin*>(img + kvc::pack_joins_offset(info.n_items + info.n_short));
+  int64_t row0 = 0, n = 0, ns = info.n_items, nj = 0, np = 0;
   for (int32_t s = 0; s < P->n_seqs; ++s) {
     const int32_t len = P->seq_len[s];
     for (int64_t b = 0, nb = pack_blocks(len, group); b < nb; ++b) {
-      const int tiles = pack_tiles(len, group, b), parts = pack_parts(tiles, info.share);
+      const int tiles = pack_tiles(len, group, b);
+      if (len <= kvc::kPackShort) {
+        items[ns++] = {(int32_t)row0, len, (int32_t)b, 0, tiles, -1, {0, 0}};
+        continue;
+      }
+      const int parts = pack_parts(tiles, info.share);
       if (parts > 1) joins[nj++] = {(int32_t)row0, len, (int32_t)b, (int32_t)np, parts, {0, 0, 0}};
       for (int i = 0; i < parts; ++i) {
         const int t0 = (int)((int64_t)tiles * i / parts), t1 = (int)((int64_t)tiles * (i + 1) / parts);
@@ -1366,7 +1378,9 @@ void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
     }
     row0 += len;
   }
-  std::stable_sort(items, items + n, [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; });
+  const auto longer = [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; };
+  std::stable_sort(items, items + n, longer);
+  std::stable_sort(items + n, items + ns, longer);
 }
 
 }  // namespace
@@ -1460,7 +1474,7 @@ kvc_status kvc_packed_attention(const kvc_pack* P, const kvc_plan* plan, const v
   if (st != KVC_OK) return st;
   const float scale = softmax_scale > 0.0f ? softmax_scale : 1.0f / std::sqrt((float)P->head_dim);
   const hipError_t e = kvc::launch_packed_attention(
-      plan->device, id, (int)i.n_items, (int)i.n_joins, (int)i.n_parts, static_cast<const uint16_t*>(q),
+      plan->device, id, (int)i.n_items, (int)i.n_short, (int)i.n_joins, (int)i.n_parts, static_cast<const uint16_t*>(q),
       static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), P->n_q_heads, P->n_kv_heads, scale,
       static_cast<uint16_t*>(out), lse, ws, as_stream(stream));
   return e != hipSuccess ? hip_fail(W, e) : ok();

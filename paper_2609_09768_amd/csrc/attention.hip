@@ -701,6 +701,185 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     P.lse[qi * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
 }
 
+// Packed sequences of up to kPackShort rows: the same units, four a workgroup of
+// four waves, two workgroups a CU.  Such a block has few key tiles, and what
+// comes before and after them (its queries, the first tile, the output) is
+// most of its time; with two workgroups a CU one's waits lie beside the other's
+// products, which is why the tiles here go through two slots and a plain loop.
+constexpr int kShortWaves = 4;
+static_assert(kShortWaves == kPackShortUnits && kWaves == kPackUnits, "the plan's blocks");
+__global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const AttnParams P) {
+  __shared__ __attribute__((aligned(16))) uint16_t K0[kKSlot], K1[kKSlot];
+  __shared__ __attribute__((aligned(16))) uint16_t V0[kVSlot], V1[kVSlot];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ql = lane & 31, half = lane >> 5;
+  const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
+  const PackItem item = P.items[blockIdx.x / (unsigned)P.n_kv_heads];
+  if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
+  const int unit = kShortWaves * item.block + wave;
+  const int sub = unit / P.group, h = g * P.group + unit % P.group;
+  const int qi = 32 * sub + ql;
+  const bool in_range = qi < item.len;
+  const long long row0 = item.row0;
+  const int n_tiles = item.n_tiles;
+
+  uint4 qraw[8];
+  {  // (a lane past the sequence takes its last query; its results go nowhere)
+    const uint16_t* qp = P.q + ((row0 + min(qi, item.len - 1)) * P.n_q_heads + h) * (long long)kHeadDim + half * 8;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) qraw[ks] = *reinterpret_cast<const uint4*>(qp + ks * 16);
+  }
+  // tiles as in sparse_attn_kernel, wave w loading rows 16 w .. 16 w + 15;
+  // rows past the sequence and tiles past the last arrive as zeros
+  const long long row_bytes = (long long)P.n_kv_heads * kHeadDim * 2;
+  const char* kbase = reinterpret_cast<const char*>(P.k) + row0 * row_bytes;
+  const char* vbase = reinterpret_cast<const char*>(P.v) + row0 * row_bytes;
+  int koff[4], voff[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 16 * wave + 4 * j + (lane >> 4), slot = lane & 15;
+    koff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (r & 3));
+    voff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (4 * (r & 3)));
+  }
+  auto load_tile = [&](int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
+    const long long r0 = (long long)t * kBN;
+    const int nbytes = (t < n_tiles ? min(kBN, item.len - t * kBN) : 0) * (int)row_bytes;
+    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (4 * wave + j) * kKGroup), 16, koff[j], 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (16 * wave + 4 * j) * kHeadDim), 16, voff[j], 0, 0, 0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  load_tile(0, K0, V0);
+  load_tile(1, K1, V1);
+  bf16x8 qreg[8];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    uint32_t a = qraw[ks].x, b = qraw[ks].y, c = qraw[ks].z, d = qraw[ks].w;
+    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+    qreg[ks] = as_bf16x8(make_uint4(a, b, c, d));
+  }
+  const int k_a0 = (ql >> 2) * kKGroup + (lane & 3) * kHeadDim + 8 * (half ^ (lane & 1));
+  const int k_e1 = 16 * ((lane >> 1) & 1);
+  const int k_rd[2] = {k_a0 + k_e1, k_a0 - k_e1};
+  int v_rd[4];
+  {
+    const int i = lane & 15, gd = (lane >> 4) & 1, sr = i >> 2;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+      v_rd[dt] = (4 * half + sr) * kHeadDim + 32 * (dt ^ sr) + 16 * gd + 4 * (i & 3);
+  }
+  f32x16 o[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  auto step = [&](int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(8 | 7 << 4 | 15 << 8);  // this wave's loads of tile t, all but the next tile's eight
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // a wave whose queries all lie before the tile has nothing to do
+    if (t * kBN <= 32 * sub + 31) {
+      f32x16 s[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int kb = i >> 3, ks = i & 7;
+        const uint4 f = *reinterpret_cast<const uint4*>(ks_ + k_rd[ks & 1] + kb * 8 * kKGroup + 16 * ks);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(f), qreg[ks], ks == 0 ? f32x16{} : s[kb], 0, 0, 0);
+      }
+      const bool edge = t * kBN + kBN - 1 > 32 * sub;  // reaches past the first query
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[kb][r] *= P.scale_log2;
+          const int key = t * kBN + kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+          if (edge) s[kb][r] = key > qi ? -INFINITY : s[kb][r];
+          mx = fmaxf(mx, s[kb][r]);
+        }
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      // the offset of the exponents follows the maximum when that has left it by 2^8
+      const float m_new = mx2 > m_run + 8.f ? mx2 : m_run;
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      if (__any(m_new != m_run)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      }
+      m_run = m_new;
+      bf16x8 pb[4];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(s[kk >> 1][(kk & 1) * 8 + 2 * e] - m_use);
+          const float p1 = __builtin_amdgcn_exp2f(s[kk >> 1][(kk & 1) * 8 + 2 * e + 1] - m_use);
+          l_run += p0 + p1;
+          w[e] = pack_bf16x2(p0, p1);
+        }
+        pb[kk] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int kk = i >> 2, dt = i & 3;
+        const uint16_t* b = vs_ + v_rd[dt] + kk * 16 * kHeadDim;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b + 8 * kHeadDim));
+        const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pb[kk], o[dt], 0, 0, 0);
+      }
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);  // reads of the slot are done
+    __builtin_amdgcn_s_barrier();
+    load_tile(t + 2, ks_, vs_);
+  };
+  for (int t = 0; t < n_tiles; t += 2) {
+    step(t, K0, V0);
+    step(t + 1, K1, V1);  // past the last tile: skipped by every wave
+  }
+
+  // whole rows through LDS, as in sparse_attn_kernel
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  __builtin_amdgcn_s_waitcnt(0 | 7 << 4);
+  __builtin_amdgcn_s_barrier();
+  uint16_t* const rows = (wave < 2 ? K0 : K1) + (wave & 1) * (32 * 136);
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr)
+      *reinterpret_cast<uint2*>(rows + ql * 136 + dt * 32 + rr * 8 + half * 4) =
+          make_uint2(pack_bf16x2(o[dt][rr * 4 + 0] * inv, o[dt][rr * 4 + 1] * inv),
+                     pack_bf16x2(o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv));
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int r = 4 * j + (lane >> 4);
+    const uint4 line = *reinterpret_cast<const uint4*>(rows + r * 136 + 8 * (lane & 15));
+    if (32 * sub + r < item.len)
+      *reinterpret_cast<uint4*>(P.out + ((row0 + 32 * sub + r) * P.n_q_heads + h) * (long long)kHeadDim + 8 * (lane & 15)) = line;
+  }
+  if (P.lse && half == 0 && in_range)
+    P.lse[(row0 + qi) * P.n_q_heads + h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+}
+
 // Merge of the split partials of one unit's queries, one wave per 32 channels
 // of a unit, read in the layout they were written in: weights 2^(lse_s - max)
 // in split order, so the result is deterministic; a query with no visible key
@@ -933,10 +1112,9 @@ hipError_t launch_attention(const uint16_t* q, int64_t n_q_rows, const int32_t* 
   return launch_combine(P, s);
 }
 
-hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_joins, int n_parts,
+hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_short, int n_joins, int n_parts,
                                    const uint16_t* q, const uint16_t* k, const uint16_t* v, int n_q_heads,
                                    int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws, hipStream_t s) {
-  if (n_items <= 0) return hipSuccess;
   AttnParams P = {};
   P.q = q;
   P.k = k;
@@ -952,17 +1130,28 @@ hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, i
   const char* base = static_cast<const char*>(plan);
   P.plan = reinterpret_cast<const PackHeader*>(base);
   P.items = reinterpret_cast<const PackItem*>(base + pack_items_offset());
-  P.joins = reinterpret_cast<const PackJoin*>(base + pack_joins_offset(n_items));
+  P.joins = reinterpret_cast<const PackJoin*>(base + pack_joins_offset((int64_t)n_items + n_short));
   P.plan_id = id;
   P.part_o = static_cast<float*>(ws);
   P.part_lse = P.part_o + (size_t)n_parts * n_kv_heads * kWaves * 32 * kHeadDim;
-  hipLaunchKernelGGL((sparse_attn_kernel<kWaves, Rows::kPacked>), dim3((unsigned)n_items * (unsigned)n_kv_heads), dim3(kThreads),
-                     0, s, P);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || n_joins == 0) return e;
-  hipLaunchKernelGGL(pack_join_kernel, dim3((unsigned)n_joins * kWaves * (unsigned)n_kv_heads), dim3(kCombineThreads), 0,
-                     s, P);
-  return hipGetLastError();
+  if (n_items > 0) {
+    hipLaunchKernelGGL((sparse_attn_kernel<kWaves, Rows::kPacked>), dim3((unsigned)n_items * (unsigned)n_kv_heads),
+                       dim3(kThreads), 0, s, P);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (n_joins > 0) {
+    hipLaunchKernelGGL(pack_join_kernel, dim3((unsigned)n_joins * kWaves * (unsigned)n_kv_heads), dim3(kCombineThreads),
+                       0, s, P);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (n_short > 0) {
+    P.items += n_items;
+    hipLaunchKernelGGL(pack_short_kernel, dim3((unsigned)n_short * (unsigned)n_kv_heads), dim3(64 * kShortWaves), 0, s, P);
+    return hipGetLastError();
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_prefix_rows(const uint16_t* q, int64_t rows, int n_q_heads, int n_kv_heads, const uint16_t* k,

@@ -207,12 +207,17 @@ hipError_t launch_prefix_rows(const uint16_t* q, int64_t rows, int n_q_heads, in
                               hipStream_t s);
 
 // ---- packed sequences (attention.hip) -----------------------------------------------
-// Work of one workgroup and kv head: eight units (32 queries of one head each)
-// of one sequence over key tiles tile0 .. tile0 + n_tiles - 1.  part: where
-// its partial results go, -1 if it has all of the keys.
+// Sequences of up to kPackShort rows have workgroups of four units (32 queries
+// of one head each), longer ones of eight.
+constexpr int kPackShort = 512;
+constexpr int kPackShortUnits = 4;
+constexpr int kPackUnits = 8;
+// Work of one workgroup and kv head: a block of units of one sequence over key
+// tiles tile0 .. tile0 + n_tiles - 1.  part: where its partial results go, -1
+// if it has all of the keys (as in every short sequence).
 struct PackItem {
   int32_t row0, len;     // the sequence's first row and its rows
-  int32_t block;         // its units are 8 block .. 8 block + 7
+  int32_t block;         // its units are 8 (4) block and those after it
   int32_t tile0, n_tiles;
   int32_t part;
   int32_t pad[2];
@@ -224,7 +229,7 @@ struct PackJoin {
 };
 struct PackHeader {
   uint64_t id;
-  int32_t n_items, n_joins, n_parts, pad;
+  int32_t n_items, n_short, n_joins, n_parts;  // items of long sequences first
 };
 inline size_t pack_items_offset() { return align256(sizeof(PackHeader)); }
 inline size_t pack_joins_offset(int64_t n_items) {
@@ -234,7 +239,7 @@ inline size_t pack_joins_offset(int64_t n_items) {
 inline size_t pack_ws_bytes(int64_t n_parts, int n_kv_heads) {
   return align256(size_t(n_parts) * size_t(n_kv_heads) * 8 * 32 * (kHeadDim + 1) * sizeof(float));
 }
-hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_joins, int n_parts,
+hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, int n_short, int n_joins, int n_parts,
                                    const uint16_t* q, const uint16_t* k, const uint16_t* v, int n_q_heads,
                                    int n_kv_heads, float scale, uint16_t* out, float* lse, void* ws, hipStream_t s);
 

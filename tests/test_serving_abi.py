@@ -113,19 +113,21 @@ def test_plan_image_covers_every_tile_once(K, lens, hq, hkv):
         pytest.skip("the upload would go to a fake address")
     img = np.zeros(nb, np.uint8)
     assert _status(K.kvc_pack_plan_upload, pack, A, nb, staging=img.ctypes.data)[0] == K.KVC_ERR_DEVICE
-    n_items, n_joins, n_parts = img[8:20].view(np.int32)
+    n_long, n_short, n_joins, n_parts = img[8:24].view(np.int32)
+    n_items = n_long + n_short
     items = img[256:256 + 32 * n_items].view(np.int32).reshape(n_items, 8)
     j0 = 256 + (32 * n_items + 255) // 256 * 256
     joins = img[j0:j0 + 32 * n_joins].view(np.int32).reshape(n_joins, 8)
-    assert (np.diff(items[:, 4]) <= 0).all()
+    assert (items[:n_long, 1] > 512).all() and (items[n_long:, 1] <= 512).all()
+    assert (np.diff(items[:n_long, 4]) <= 0).all() and (np.diff(items[n_long:, 4]) <= 0).all()
     grp, row0, seen = hq // hkv, 0, 0
     parts = {}
     for r, n, b, t0, nt, part in items[:, :6]:
         parts.setdefault((int(r), int(n), int(b)), []).append((int(t0), int(nt), int(part)))
     for n in lens:
-        units = -(-n // 32) * grp
-        for b in range(-(-units // 8)):
-            last = min(32 * ((8 * b + 7) // grp + 1), n) - 1
+        units, wide = -(-n // 32) * grp, 8 if n > 512 else 4
+        for b in range(-(-units // wide)):
+            last = min(32 * ((wide * b + wide - 1) // grp + 1), n) - 1
             got = sorted(parts.pop((row0, n, b)))
             at = 0
             for t0, nt, part in got:
