@@ -1347,7 +1347,8 @@ size_t pack_bytes(const PackInfo& i) {
   return kvc::pack_joins_offset(i.n_items + i.n_short) + kvc::align256(sizeof(kvc::PackJoin) * (size_t)i.n_joins);
 }
 
-// The plan's image: work items, those with the most tiles first.
+// The plan's image: work items, those with the most tiles (of short sequences,
+// the longest sequences) first.
 void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
   const int group = P->n_q_heads / P->n_kv_heads;
   kvc::PackHeader hdr;
@@ -1378,9 +1379,11 @@ void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
     }
     row0 += len;
   }
-  const auto longer = [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; };
-  std::stable_sort(items, items + n, longer);
-  std::stable_sort(items + n, items + ns, longer);
+  std::stable_sort(items, items + n, [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; });
+  // a short sequence's blocks together, so that they find its keys in L2
+  std::stable_sort(items + n, items + ns, [](const kvc::PackItem& a, const kvc::PackItem& b) {
+    return a.len != b.len ? a.len > b.len : a.row0 != b.row0 ? a.row0 < b.row0 : a.block > b.block;
+  });
 }
 
 }  // namespace

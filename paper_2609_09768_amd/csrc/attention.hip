@@ -703,70 +703,90 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 
 // Packed sequences of up to kPackShort rows: the same units, four a workgroup of
 // four waves, two workgroups a CU.  Such a block has few key tiles, and what
-// comes before and after them (its queries, the first tile, the output) is
-// most of its time; with two workgroups a CU one's waits lie beside the other's
-// products, which is why the tiles here go through two slots and a plain loop.
+// comes before and after them (its work item, its queries, the first tiles, the
+// output) would be most of its time.  So the workgroups stay and take one block
+// after the other (every gridDim-th; the longest come first, so the shares are
+// even), the next block's first two tiles are asked for beside the last two of
+// the present one and its queries beside the output, and one workgroup's waits lie beside the
+// other's products.  Tiles go through two slots and a plain loop.
 constexpr int kShortWaves = 4;
 static_assert(kShortWaves == kPackShortUnits && kWaves == kPackUnits, "the plan's blocks");
-__global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const AttnParams P) {
+constexpr int kShortRow = 40;  // bf16 between rows of 32 channels on their way out
+__global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const AttnParams P, int n_items) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[kKSlot], K1[kKSlot];
   __shared__ __attribute__((aligned(16))) uint16_t V0[kVSlot], V1[kVSlot];
+  __shared__ __attribute__((aligned(16))) uint16_t out_rows[kShortWaves * 32 * kShortRow];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ql = lane & 31, half = lane >> 5;
-  const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
-  const PackItem item = P.items[blockIdx.x / (unsigned)P.n_kv_heads];
+  const unsigned n_all = (unsigned)n_items * (unsigned)P.n_kv_heads;
   if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
-  const int unit = kShortWaves * item.block + wave;
-  const int sub = unit / P.group, h = g * P.group + unit % P.group;
-  const int qi = 32 * sub + ql;
-  const bool in_range = qi < item.len;
-  const long long row0 = item.row0;
-  const int n_tiles = item.n_tiles;
 
+  // a block, the same in every lane
+  struct Block {
+    int g, len, sub, h, n_tiles;
+    long long row0;
+  };
+  auto block_at = [&](unsigned i) __attribute__((always_inline)) {
+    typedef __attribute__((address_space(4))) const PackItem const_item;
+    const const_item* it = (const const_item*)(uintptr_t)(P.items + i / (unsigned)P.n_kv_heads);
+    const int unit = kShortWaves * it->block + wave;
+    Block b;
+    b.g = (int)(i % (unsigned)P.n_kv_heads);
+    b.len = it->len;
+    b.sub = unit / P.group;
+    b.h = b.g * P.group + unit % P.group;
+    b.n_tiles = it->n_tiles;
+    b.row0 = it->row0;
+    return b;
+  };
   uint4 qraw[8];
-  {  // (a lane past the sequence takes its last query; its results go nowhere)
-    const uint16_t* qp = P.q + ((row0 + min(qi, item.len - 1)) * P.n_q_heads + h) * (long long)kHeadDim + half * 8;
+  auto load_q = [&](const Block& b) __attribute__((always_inline)) {
+    // (a lane past the sequence takes its last query; its results go nowhere)
+    const uint16_t* qp =
+        P.q + ((b.row0 + min(32 * b.sub + ql, b.len - 1)) * P.n_q_heads + b.h) * (long long)kHeadDim + half * 8;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) qraw[ks] = *reinterpret_cast<const uint4*>(qp + ks * 16);
-  }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The 64 lines of a block's queries for this wave, a lane each, brought to L2
+  // for the loads above (which would need 32 registers this early).
+  uint32_t touched = 0;
+  auto touch_q = [&](const Block& b) __attribute__((always_inline)) {
+    touched = *reinterpret_cast<const uint32_t*>(
+        P.q + ((b.row0 + min(32 * b.sub + ql, b.len - 1)) * P.n_q_heads + b.h) * (long long)kHeadDim + half * 64);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
   // tiles as in sparse_attn_kernel, wave w loading rows 16 w .. 16 w + 15;
   // rows past the sequence and tiles past the last arrive as zeros
   const long long row_bytes = (long long)P.n_kv_heads * kHeadDim * 2;
-  const char* kbase = reinterpret_cast<const char*>(P.k) + row0 * row_bytes;
-  const char* vbase = reinterpret_cast<const char*>(P.v) + row0 * row_bytes;
   int koff[4], voff[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = 16 * wave + 4 * j + (lane >> 4), slot = lane & 15;
-    koff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (r & 3));
-    voff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (4 * (r & 3)));
+    koff[j] = (int)(r * row_bytes) + 16 * (slot ^ (r & 3));
+    voff[j] = (int)(r * row_bytes) + 16 * (slot ^ (4 * (r & 3)));
   }
-  auto load_tile = [&](int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
-    const long long r0 = (long long)t * kBN;
-    const int nbytes = (t < n_tiles ? min(kBN, item.len - t * kBN) : 0) * (int)row_bytes;
-    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
+  auto load_tile = [&](const Block& b, int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
+    const long long at = (b.row0 + (long long)t * kBN) * row_bytes;
+    // (a head's last row ends 256 bytes times the heads after it before the row does)
+    const int nbytes = (t < b.n_tiles ? min(kBN, b.len - t * kBN) : 0) * (int)row_bytes;
+    const int goff = b.g * kHeadDim * 2;
+    const __amdgpu_buffer_rsrc_t rk =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const char*>(P.k) + at), (short)0, nbytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const char*>(P.v) + at), (short)0, nbytes, 0x00020000);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (4 * wave + j) * kKGroup), 16, koff[j], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (4 * wave + j) * kKGroup), 16, koff[j] + goff, 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (16 * wave + 4 * j) * kHeadDim), 16, voff[j], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (16 * wave + 4 * j) * kHeadDim), 16, voff[j] + goff, 0, 0, 0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  load_tile(0, K0, V0);
-  load_tile(1, K1, V1);
-  bf16x8 qreg[8];
-#pragma unroll
-  for (int ks = 0; ks < 8; ++ks) {
-    uint32_t a = qraw[ks].x, b = qraw[ks].y, c = qraw[ks].z, d = qraw[ks].w;
-    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
-    qreg[ks] = as_bf16x8(make_uint4(a, b, c, d));
-  }
   const int k_a0 = (ql >> 2) * kKGroup + (lane & 3) * kHeadDim + 8 * (half ^ (lane & 1));
   const int k_e1 = 16 * ((lane >> 1) & 1);
   const int k_rd[2] = {k_a0 + k_e1, k_a0 - k_e1};
@@ -777,44 +797,58 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
     for (int dt = 0; dt < 4; ++dt)
       v_rd[dt] = (4 * half + sr) * kHeadDim + 32 * (dt ^ sr) + 16 * gd + 4 * (i & 3);
   }
-  f32x16 o[4];
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
 
-  auto step = [&](int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(8 | 7 << 4 | 15 << 8);  // this wave's loads of tile t, all but the next tile's eight
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    // a wave whose queries all lie before the tile has nothing to do
-    if (t * kBN <= 32 * sub + 31) {
-      f32x16 s[2];
+  Block cur = block_at(blockIdx.x);
+  load_q(cur);
+  load_tile(cur, 0, K0, V0);
+  load_tile(cur, 1, K1, V1);
+  for (unsigned idx = blockIdx.x;; idx += gridDim.x) {
+    const bool more = idx + gridDim.x < n_all;
+    Block next = block_at(more ? idx + gridDim.x : idx);
+    if (!more) next.n_tiles = 0;  // its tiles are zeros
+    // queries and first tiles of this block (and the last one's stores)
+    __builtin_amdgcn_s_waitcnt(0 | 7 << 4 | 15 << 8);
+    bf16x8 qreg[8];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+    for (int ks = 0; ks < 8; ++ks) qreg[ks] = as_bf16x8(qraw[ks]);
+    const int qi = 32 * cur.sub + ql;
+    f32x16 o[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // Products of a tile's first HALVES x 32 keys: half of it where the wave's
+    // queries end there.
+    auto products_of = [&](auto halves, int t, const uint16_t* ks_, const uint16_t* vs_) __attribute__((always_inline)) {
+      constexpr int HALVES = decltype(halves)::value;
+      f32x16 s[HALVES];
+#pragma unroll
+      for (int i = 0; i < 8 * HALVES; ++i) {
         const int kb = i >> 3, ks = i & 7;
         const uint4 f = *reinterpret_cast<const uint4*>(ks_ + k_rd[ks & 1] + kb * 8 * kKGroup + 16 * ks);
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(f), qreg[ks], ks == 0 ? f32x16{} : s[kb], 0, 0, 0);
       }
-      const bool edge = t * kBN + kBN - 1 > 32 * sub;  // reaches past the first query
-      float mx = -INFINITY;
+      if (t * kBN + 32 * HALVES - 1 > 32 * cur.sub) {  // reaches past the wave's first query
+        const int behind = qi - t * kBN - half * 4;    // keys up to this one, from the lane's first
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < HALVES; ++kb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[kb][r] *= P.scale_log2;
-          const int key = t * kBN + kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          if (edge) s[kb][r] = key > qi ? -INFINITY : s[kb][r];
-          mx = fmaxf(mx, s[kb][r]);
-        }
+          for (int r = 0; r < 16; ++r) s[kb][r] = kb * 32 + (r >> 2) * 8 + (r & 3) > behind ? -INFINITY : s[kb][r];
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < HALVES; ++kb)
+#pragma unroll
+        for (int r = kb == 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      // (every query sees a key of tile 0, so the maximum is finite from then on)
+      const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * P.scale_log2;
       // the offset of the exponents follows the maximum when that has left it by 2^8
       const float m_new = mx2 > m_run + 8.f ? mx2 : m_run;
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;
-      if (__any(m_new != m_run)) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      if (__any(m_new != m_run && t > 0)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -822,21 +856,21 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
           for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
       }
       m_run = m_new;
-      bf16x8 pb[4];
+      bf16x8 pb[2 * HALVES];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
+      for (int kk = 0; kk < 2 * HALVES; ++kk) {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p0 = __builtin_amdgcn_exp2f(s[kk >> 1][(kk & 1) * 8 + 2 * e] - m_use);
-          const float p1 = __builtin_amdgcn_exp2f(s[kk >> 1][(kk & 1) * 8 + 2 * e + 1] - m_use);
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e], P.scale_log2, -m_new));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e + 1], P.scale_log2, -m_new));
           l_run += p0 + p1;
           w[e] = pack_bf16x2(p0, p1);
         }
         pb[kk] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8 * HALVES; ++i) {
         const int kk = i >> 2, dt = i & 3;
         const uint16_t* b = vs_ + v_rd[dt] + kk * 16 * kHeadDim;
         const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(b));
@@ -844,40 +878,70 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
         const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
         o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), pb[kk], o[dt], 0, 0, 0);
       }
+    };
+    auto products = [&](int t, const uint16_t* ks_, const uint16_t* vs_) __attribute__((always_inline)) {
+      if (cur.sub > 2 * t) products_of(std::integral_constant<int, 2>{}, t, ks_, vs_);
+      else if (cur.sub == 2 * t) products_of(std::integral_constant<int, 1>{}, t, ks_, vs_);
+      // a wave whose queries all lie before the tile has nothing to do
+    };
+    // the slot has been read by every wave
+    auto done = [&]() __attribute__((always_inline)) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    // Tiles in pairs (a second one past the last is skipped by every wave).
+    // Loads return in order: behind a tile's own eight, the next tile's eight
+    // may be under way, and behind the first tile of a pair the touch.
+    for (int t = 0; t < cur.n_tiles; t += 2) {
+      const bool last = t + 2 >= cur.n_tiles;
+      __builtin_amdgcn_s_waitcnt(8 | 7 << 4 | 15 << 8);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      products(t, K0, V0);
+      done();
+      load_tile(last ? next : cur, last ? 0 : t + 2, K0, V0);
+      touch_q(last ? next : cur);
+      __builtin_amdgcn_s_waitcnt(9 | 7 << 4 | 15 << 8);
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      products(t + 1, K1, V1);
+      done();
+      load_tile(last ? next : cur, last ? 1 : t + 3, K1, V1);
     }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);  // reads of the slot are done
-    __builtin_amdgcn_s_barrier();
-    load_tile(t + 2, ks_, vs_);
-  };
-  for (int t = 0; t < n_tiles; t += 2) {
-    step(t, K0, V0);
-    step(t + 1, K1, V1);  // past the last tile: skipped by every wave
-  }
 
-  // whole rows through LDS, as in sparse_attn_kernel
-  const float l_tot = l_run + __shfl_xor(l_run, 32);
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-  __builtin_amdgcn_s_waitcnt(0 | 7 << 4);
-  __builtin_amdgcn_s_barrier();
-  uint16_t* const rows = (wave < 2 ? K0 : K1) + (wave & 1) * (32 * 136);
+    load_q(next);
+    asm volatile("" ::"v"(touched));
+    // Whole pieces of rows through LDS, 32 channels at a time: 64 bytes of 16
+    // rows per store.
+    const float l_tot = l_run + __shfl_xor(l_run, 32);
+    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    uint16_t* const rows = out_rows + wave * 32 * kShortRow;
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
+    for (int dt = 0; dt < 4; ++dt) {
 #pragma unroll
-    for (int rr = 0; rr < 4; ++rr)
-      *reinterpret_cast<uint2*>(rows + ql * 136 + dt * 32 + rr * 8 + half * 4) =
-          make_uint2(pack_bf16x2(o[dt][rr * 4 + 0] * inv, o[dt][rr * 4 + 1] * inv),
-                     pack_bf16x2(o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv));
-  __builtin_amdgcn_wave_barrier();
+      for (int rr = 0; rr < 4; ++rr)
+        *reinterpret_cast<uint2*>(rows + ql * kShortRow + rr * 8 + half * 4) =
+            make_uint2(pack_bf16x2(o[dt][rr * 4 + 0] * inv, o[dt][rr * 4 + 1] * inv),
+                       pack_bf16x2(o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv));
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int r = 4 * j + (lane >> 4);
-    const uint4 line = *reinterpret_cast<const uint4*>(rows + r * 136 + 8 * (lane & 15));
-    if (32 * sub + r < item.len)
-      *reinterpret_cast<uint4*>(P.out + ((row0 + 32 * sub + r) * P.n_q_heads + h) * (long long)kHeadDim + 8 * (lane & 15)) = line;
+      for (int j = 0; j < 2; ++j) {
+        const int r = 16 * j + (lane >> 2);
+        const uint4 piece = *reinterpret_cast<const uint4*>(rows + r * kShortRow + 8 * (lane & 3));
+        if (32 * cur.sub + r < cur.len)
+          *reinterpret_cast<uint4*>(P.out + ((cur.row0 + 32 * cur.sub + r) * P.n_q_heads + cur.h) * (long long)kHeadDim +
+                                    32 * dt + 8 * (lane & 3)) = piece;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    if (P.lse && half == 0 && qi < cur.len)
+      P.lse[(cur.row0 + qi) * P.n_q_heads + cur.h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+    if (!more) break;
+    cur = next;
   }
-  if (P.lse && half == 0 && in_range)
-    P.lse[(row0 + qi) * P.n_q_heads + h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+  __builtin_amdgcn_s_waitcnt(0 | 7 << 4 | 15 << 8);  // no load is left to write into LDS
 }
 
 // Merge of the split partials of one unit's queries, one wave per 32 channels
@@ -1148,7 +1212,10 @@ hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, i
   }
   if (n_short > 0) {
     P.items += n_items;
-    hipLaunchKernelGGL(pack_short_kernel, dim3((unsigned)n_short * (unsigned)n_kv_heads), dim3(64 * kShortWaves), 0, s, P);
+    // two workgroups a CU, in whole rounds of the kv heads: a workgroup keeps its head
+    const unsigned blocks = (unsigned)n_short * (unsigned)n_kv_heads;
+    const unsigned most = std::max(2u * kCus / (unsigned)n_kv_heads, 1u) * (unsigned)n_kv_heads;
+    hipLaunchKernelGGL(pack_short_kernel, dim3(std::min(blocks, most)), dim3(64 * kShortWaves), 0, s, P, n_short);
     return hipGetLastError();
   }
   return hipSuccess;

@@ -119,7 +119,7 @@ def test_plan_image_covers_every_tile_once(K, lens, hq, hkv):
     j0 = 256 + (32 * n_items + 255) // 256 * 256
     joins = img[j0:j0 + 32 * n_joins].view(np.int32).reshape(n_joins, 8)
     assert (items[:n_long, 1] > 512).all() and (items[n_long:, 1] <= 512).all()
-    assert (np.diff(items[:n_long, 4]) <= 0).all() and (np.diff(items[n_long:, 4]) <= 0).all()
+    assert (np.diff(items[:n_long, 4]) <= 0).all() and (np.diff(items[n_long:, 1]) <= 0).all()
     grp, row0, seen = hq // hkv, 0, 0
     parts = {}
     for r, n, b, t0, nt, part in items[:, :6]:
