@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <algorithm>
 #include <cstring>
+#include <functional>
 #include <initializer_list>
 #include <string>
 #include <vector>
@@ -1280,8 +1281,11 @@ int pack_tiles(int64_t len, int group, int64_t block) {
 // takes about the larger of a CU's share of all tiles and the longest block:
 // one that is a quarter longer than the share is cut into parts of about the
 // share, but of no less than kPackLeast tiles, since a workgroup costs about as
-// much as that before and after its tiles.
-constexpr int kPackLeast = 8;
+// much as ten of them before and after its own, and its parts are joined by
+// one more launch (one sequence of 1,500 rows of 32/8 heads 40 us with at least
+// 8 tiles, 37 with 16, 35 with 24; three of 3,000 of 4/1 heads 46 with 16, 49
+// with 24).
+constexpr int kPackLeast = 16;
 int pack_parts(int tiles, int64_t share) {
   const int64_t part = std::max<int64_t>(share, kPackLeast);
   return 4 * (int64_t)tiles > 5 * part ? (int)((tiles + part - 1) / part) : 1;
@@ -1343,8 +1347,9 @@ uint64_t pack_id(const kvc_pack* P) {
   return h | 1ull;
 }
 
-size_t pack_bytes(const PackInfo& i) {
-  return kvc::pack_joins_offset(i.n_items + i.n_short) + kvc::align256(sizeof(kvc::PackJoin) * (size_t)i.n_joins);
+size_t pack_bytes(const PackInfo& i, int n_kv_heads) {
+  return kvc::pack_queues_offset(i.n_items + i.n_short, i.n_joins) +
+         kvc::align256(sizeof(int32_t) * (size_t)(kvc::pack_queues(i.n_short, n_kv_heads) + 1));
 }
 
 // The plan's image: work items, those with the most tiles (of short sequences,
@@ -1380,10 +1385,31 @@ void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
     row0 += len;
   }
   std::stable_sort(items, items + n, [](const kvc::PackItem& a, const kvc::PackItem& b) { return a.n_tiles > b.n_tiles; });
-  // a short sequence's blocks together, so that they find its keys in L2
-  std::stable_sort(items + n, items + ns, [](const kvc::PackItem& a, const kvc::PackItem& b) {
+  // Short sequences: the longest first, a sequence's blocks together so that
+  // they find its keys in L2, each block to the queue with the least to do
+  // (its tiles, and about two tiles' time for its queries and output).
+  kvc::PackItem* const first = items + n;
+  std::stable_sort(first, items + ns, [](const kvc::PackItem& a, const kvc::PackItem& b) {
     return a.len != b.len ? a.len > b.len : a.row0 != b.row0 ? a.row0 < b.row0 : a.block > b.block;
   });
+  const int64_t queues = kvc::pack_queues(info.n_short, P->n_kv_heads);
+  int32_t* start = reinterpret_cast<int32_t*>(img + kvc::pack_queues_offset(info.n_items + info.n_short, info.n_joins));
+  std::vector<std::pair<int64_t, int32_t>> load((size_t)queues);  // heap, the least first, then the lowest number
+  for (int64_t i = 0; i < queues; ++i) load[(size_t)i] = {0, (int32_t)i};
+  std::vector<int32_t> queue((size_t)info.n_short);
+  std::vector<int32_t> count((size_t)queues + 1, 0);
+  for (int64_t i = 0; i < info.n_short; ++i) {
+    std::pop_heap(load.begin(), load.end(), std::greater<>());
+    std::pair<int64_t, int32_t>& q = load.back();
+    queue[(size_t)i] = q.second;
+    ++count[(size_t)q.second + 1];
+    q.first += first[i].n_tiles + 2;
+    std::push_heap(load.begin(), load.end(), std::greater<>());
+  }
+  for (int64_t i = 0; i < queues; ++i) count[(size_t)i + 1] += count[(size_t)i];
+  for (int64_t i = 0; i <= queues; ++i) start[i] = count[(size_t)i];
+  const std::vector<kvc::PackItem> sorted(first, items + ns);
+  for (int64_t i = 0; i < info.n_short; ++i) first[count[(size_t)queue[(size_t)i]]++] = sorted[(size_t)i];
 }
 
 }  // namespace
@@ -1396,7 +1422,7 @@ kvc_status kvc_pack_plan_bytes(const kvc_pack* P, size_t* bytes) {
   const kvc_status st = check_pack(W, P, &i);
   if (st != KVC_OK) return st;
   if (!bytes) return fail(KVC_ERR_INVALID_ARG, "%s: bytes is NULL", W);
-  *bytes = pack_bytes(i);
+  *bytes = pack_bytes(i, P->n_kv_heads);
   return ok();
 }
 
@@ -1408,7 +1434,7 @@ kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_b
   if (st != KVC_OK) return st;
   if (!plan_dev || !aligned16(plan_dev)) return fail(KVC_ERR_INVALID_ARG, "%s: plan is NULL or not 16-byte aligned", W);
   if (!plan_out) return fail(KVC_ERR_INVALID_ARG, "%s: plan_out is NULL", W);
-  const size_t need = pack_bytes(info);
+  const size_t need = pack_bytes(info, P->n_kv_heads);
   if (plan_bytes_in < need)
     return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan_bytes_in, need);
   std::vector<unsigned char> own;
@@ -1459,8 +1485,8 @@ kvc_status kvc_packed_attention(const kvc_pack* P, const kvc_plan* plan, const v
   if (plan->layout_id != id)
     return fail(KVC_ERR_INVALID_ARG, "%s: the plan was built for other sequences (id %016llx, these %016llx)", W,
                 (unsigned long long)plan->layout_id, (unsigned long long)id);
-  if (plan->bytes < pack_bytes(i))
-    return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan->bytes, pack_bytes(i));
+  if (plan->bytes < pack_bytes(i, P->n_kv_heads))
+    return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan->bytes, pack_bytes(i, P->n_kv_heads));
   if (!q || !k || !v || !out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned4(lse))
     return fail(KVC_ERR_INVALID_ARG, "%s: NULL or misaligned pointer", W);
   const size_t need = i.n_parts > 0 ? kvc::pack_ws_bytes(i.n_parts, P->n_kv_heads) : 0;

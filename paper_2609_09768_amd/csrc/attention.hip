@@ -122,6 +122,7 @@ struct AttnParams {
   const PackHeader* plan;
   const PackItem* items;
   const PackJoin* joins;
+  const int32_t* queues;
   unsigned long long plan_id;
 };
 
@@ -704,38 +705,38 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 // Packed sequences of up to kPackShort rows: the same units, four a workgroup of
 // four waves, two workgroups a CU.  Such a block has few key tiles, and what
 // comes before and after them (its work item, its queries, the first tiles, the
-// output) would be most of its time.  So the workgroups stay and take one block
-// after the other (every gridDim-th; the longest come first, so the shares are
-// even), the next block's first two tiles are asked for beside the last two of
+// output) would be most of its time.  So the workgroups stay and take the
+// blocks of a queue of the plan one after the other, the next block's first two tiles are asked for beside the last two of
 // the present one and its queries beside the output, and one workgroup's waits lie beside the
 // other's products.  Tiles go through two slots and a plain loop.
 constexpr int kShortWaves = 4;
 static_assert(kShortWaves == kPackShortUnits && kWaves == kPackUnits, "the plan's blocks");
 constexpr int kShortRow = 40;  // bf16 between rows of 32 channels on their way out
-__global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const AttnParams P, int n_items) {
+__global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const AttnParams P) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[kKSlot], K1[kKSlot];
   __shared__ __attribute__((aligned(16))) uint16_t V0[kVSlot], V1[kVSlot];
   __shared__ __attribute__((aligned(16))) uint16_t out_rows[kShortWaves * 32 * kShortRow];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ql = lane & 31, half = lane >> 5;
-  const unsigned n_all = (unsigned)n_items * (unsigned)P.n_kv_heads;
   if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
+  const int g = (int)(blockIdx.x % (unsigned)P.n_kv_heads);
+  const int32_t* const queue = P.queues + blockIdx.x / (unsigned)P.n_kv_heads;
+  const int end = queue[1];
 
   // a block, the same in every lane
   struct Block {
-    int g, len, sub, h, n_tiles;
+    int len, sub, h, n_tiles;
     long long row0;
   };
-  auto block_at = [&](unsigned i) __attribute__((always_inline)) {
+  auto block_at = [&](int i) __attribute__((always_inline)) {
     typedef __attribute__((address_space(4))) const PackItem const_item;
-    const const_item* it = (const const_item*)(uintptr_t)(P.items + i / (unsigned)P.n_kv_heads);
+    const const_item* it = (const const_item*)(uintptr_t)(P.items + i);
     const int unit = kShortWaves * it->block + wave;
     Block b;
-    b.g = (int)(i % (unsigned)P.n_kv_heads);
     b.len = it->len;
     b.sub = unit / P.group;
-    b.h = b.g * P.group + unit % P.group;
+    b.h = g * P.group + unit % P.group;
     b.n_tiles = it->n_tiles;
     b.row0 = it->row0;
     return b;
@@ -766,24 +767,22 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = 16 * wave + 4 * j + (lane >> 4), slot = lane & 15;
-    koff[j] = (int)(r * row_bytes) + 16 * (slot ^ (r & 3));
-    voff[j] = (int)(r * row_bytes) + 16 * (slot ^ (4 * (r & 3)));
+    koff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (r & 3));
+    voff[j] = (int)(r * row_bytes) + g * kHeadDim * 2 + 16 * (slot ^ (4 * (r & 3)));
   }
   auto load_tile = [&](const Block& b, int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
     const long long at = (b.row0 + (long long)t * kBN) * row_bytes;
-    // (a head's last row ends 256 bytes times the heads after it before the row does)
     const int nbytes = (t < b.n_tiles ? min(kBN, b.len - t * kBN) : 0) * (int)row_bytes;
-    const int goff = b.g * kHeadDim * 2;
     const __amdgpu_buffer_rsrc_t rk =
         __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const char*>(P.k) + at), (short)0, nbytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t rv =
         __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const char*>(P.v) + at), (short)0, nbytes, 0x00020000);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (4 * wave + j) * kKGroup), 16, koff[j] + goff, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (4 * wave + j) * kKGroup), 16, koff[j], 0, 0, 0);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (16 * wave + 4 * j) * kHeadDim), 16, voff[j] + goff, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (16 * wave + 4 * j) * kHeadDim), 16, voff[j], 0, 0, 0);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -798,13 +797,13 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
       v_rd[dt] = (4 * half + sr) * kHeadDim + 32 * (dt ^ sr) + 16 * gd + 4 * (i & 3);
   }
 
-  Block cur = block_at(blockIdx.x);
+  Block cur = block_at(queue[0]);  // no queue is empty
   load_q(cur);
   load_tile(cur, 0, K0, V0);
   load_tile(cur, 1, K1, V1);
-  for (unsigned idx = blockIdx.x;; idx += gridDim.x) {
-    const bool more = idx + gridDim.x < n_all;
-    Block next = block_at(more ? idx + gridDim.x : idx);
+  for (int i = queue[0];; ++i) {
+    const bool more = i + 1 < end;
+    Block next = block_at(more ? i + 1 : i);
     if (!more) next.n_tiles = 0;  // its tiles are zeros
     // queries and first tiles of this block (and the last one's stores)
     __builtin_amdgcn_s_waitcnt(0 | 7 << 4 | 15 << 8);
@@ -1212,10 +1211,9 @@ hipError_t launch_packed_attention(const void* plan, uint64_t id, int n_items, i
   }
   if (n_short > 0) {
     P.items += n_items;
-    // two workgroups a CU, in whole rounds of the kv heads: a workgroup keeps its head
-    const unsigned blocks = (unsigned)n_short * (unsigned)n_kv_heads;
-    const unsigned most = std::max(2u * kCus / (unsigned)n_kv_heads, 1u) * (unsigned)n_kv_heads;
-    hipLaunchKernelGGL(pack_short_kernel, dim3(std::min(blocks, most)), dim3(64 * kShortWaves), 0, s, P, n_short);
+    P.queues = reinterpret_cast<const int32_t*>(base + pack_queues_offset((int64_t)n_items + n_short, n_joins));
+    const unsigned queues = (unsigned)pack_queues(n_short, n_kv_heads);
+    hipLaunchKernelGGL(pack_short_kernel, dim3(queues * (unsigned)n_kv_heads), dim3(64 * kShortWaves), 0, s, P);
     return hipGetLastError();
   }
   return hipSuccess;

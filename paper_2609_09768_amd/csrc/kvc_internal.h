@@ -208,8 +208,10 @@ hipError_t launch_prefix_rows(const uint16_t* q, int64_t rows, int n_q_heads, in
 
 // ---- packed sequences (attention.hip) -----------------------------------------------
 // Sequences of up to kPackShort rows have workgroups of four units (32 queries
-// of one head each), longer ones of eight.
-constexpr int kPackShort = 512;
+// of one head each), longer ones of eight: 40 sequences of 600 rows of 32/8
+// heads take 209 us in blocks of four and 231 in blocks of eight, 24 of 1,000
+// rows 285 and 275.
+constexpr int kPackShort = 768;
 constexpr int kPackShortUnits = 4;
 constexpr int kPackUnits = 8;
 // Work of one workgroup and kv head: a block of units of one sequence over key
@@ -231,9 +233,19 @@ struct PackHeader {
   uint64_t id;
   int32_t n_items, n_short, n_joins, n_parts;  // items of long sequences first
 };
+// The short sequences' items lie in the order of the queues that work on them,
+// each a workgroup for every kv head, two workgroups a CU.
+inline int64_t pack_queues(int64_t n_short, int n_kv_heads) {
+  const int64_t most = 512 / n_kv_heads;  // >= 8
+  return n_short < most ? n_short : most;
+}
 inline size_t pack_items_offset() { return align256(sizeof(PackHeader)); }
 inline size_t pack_joins_offset(int64_t n_items) {
   return pack_items_offset() + align256(sizeof(PackItem) * size_t(n_items));
+}
+// First item of each queue, and the end of the last one's.
+inline size_t pack_queues_offset(int64_t n_items, int64_t n_joins) {
+  return pack_joins_offset(n_items) + align256(sizeof(PackJoin) * size_t(n_joins));
 }
 // Partials of a part: 8 units of 32 queries, D sums and a log-sum each.
 inline size_t pack_ws_bytes(int64_t n_parts, int n_kv_heads) {

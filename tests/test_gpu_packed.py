@@ -60,7 +60,7 @@ def test_lengths_and_heads(K, lens, hq, hkv):
 # rows of 28 heads fill the GPU without that)
 @pytest.mark.parametrize("lens,hq,hkv,cut", [([2048], 4, 1, True), ([1500, 1], 1, 1, True),
                                              ([3000, 40, 2000], 8, 2, True), ([5000], 28, 4, False),
-                                             ([1025], 9, 3, True)])
+                                             ([1025], 9, 3, False), ([1400], 9, 3, True)])
 def test_cut_keys(K, lens, hq, hkv, cut):
     g = gen(sum(lens))
     n = sum(lens)

@@ -118,14 +118,21 @@ def test_plan_image_covers_every_tile_once(K, lens, hq, hkv):
     items = img[256:256 + 32 * n_items].view(np.int32).reshape(n_items, 8)
     j0 = 256 + (32 * n_items + 255) // 256 * 256
     joins = img[j0:j0 + 32 * n_joins].view(np.int32).reshape(n_joins, 8)
-    assert (items[:n_long, 1] > 512).all() and (items[n_long:, 1] <= 512).all()
-    assert (np.diff(items[:n_long, 4]) <= 0).all() and (np.diff(items[n_long:, 1]) <= 0).all()
+    assert (items[:n_long, 1] > 768).all() and (items[n_long:, 1] <= 768).all()
+    assert (np.diff(items[:n_long, 4]) <= 0).all()
+    # the short sequences' queues: two workgroups a CU, none empty, loads (tiles and two per block) nearly even
+    queues = min(int(n_short), 512 // hkv)
+    q0 = j0 + (32 * n_joins + 255) // 256 * 256
+    start = img[q0:q0 + 4 * (queues + 1)].view(np.int32)
+    assert nb >= q0 + 4 * (queues + 1) and start[0] == 0 and start[-1] == n_short and (np.diff(start) > 0).all()
+    load = [int((items[n_long + a:n_long + b, 4] + 2).sum()) for a, b in zip(start[:-1], start[1:])]
+    assert not load or max(load) - min(load) <= 10
     grp, row0, seen = hq // hkv, 0, 0
     parts = {}
     for r, n, b, t0, nt, part in items[:, :6]:
         parts.setdefault((int(r), int(n), int(b)), []).append((int(t0), int(nt), int(part)))
     for n in lens:
-        units, wide = -(-n // 32) * grp, 8 if n > 512 else 4
+        units, wide = -(-n // 32) * grp, 8 if n > 768 else 4
         for b in range(-(-units // wide)):
             last = min(32 * ((wide * b + wide - 1) // grp + 1), n) - 1
             got = sorted(parts.pop((row0, n, b)))
