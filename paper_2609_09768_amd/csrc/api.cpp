@@ -12,6 +12,7 @@
 #include <cstring>
 #include <functional>
 #include <initializer_list>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1439,13 +1440,17 @@ kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_b
     return fail(KVC_ERR_WORKSPACE, "%s: plan buffer %zu bytes, need %zu", W, plan_bytes_in, need);
   std::vector<unsigned char> own;
   unsigned char* img = static_cast<unsigned char*>(host_staging);
-  if (!img) {
-    own.assign(need, 0);
-    img = own.data();
-  } else {
-    std::memset(img, 0, need);
+  try {
+    if (!img) {
+      own.assign(need, 0);
+      img = own.data();
+    } else {
+      std::memset(img, 0, need);
+    }
+    build_pack(P, info, img);
+  } catch (const std::bad_alloc&) {
+    return fail(KVC_ERR_WORKSPACE, "%s: no host memory for a plan of %zu bytes", W, need);
   }
-  build_pack(P, info, img);
   st = need_device(W);
   if (st != KVC_OK) return st;
   hipError_t e = hipMemcpyAsync(plan_dev, img, need, hipMemcpyHostToDevice, as_stream(stream));

@@ -139,6 +139,19 @@ def test_rows_behind_a_length_may_hold_anything(K, junk):
     assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
 
 
+@pytest.mark.parametrize("slots,hkv", [(4, 2), (40, 2)])
+def test_idle_slots_may_hold_anything(K, slots, hkv):
+    # NaN and infinite queries in slots that are not in use, beside others in the same 32 rows
+    lens = [0 if i % 3 == 1 else 7 + i for i in range(slots)]
+    want = Case(K, 150, lens, 1, 8, hkv, 16, seed=12).run()
+    got = Case(K, 150, lens, 1, 8, hkv, 16, seed=12)
+    for i in range(1, slots, 3):
+        got.q[i] = 0x7FC0 if i % 2 else 0x7F80
+    got.run()
+    assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
+    got.check(slots=[0, 1, 2])
+
+
 def test_pool_past_4_gib(K):
     # pages whose byte offsets pass 32 bits
     n_pages, pr, hkv, hq = 2100, 1024, 8, 16
