@@ -149,7 +149,8 @@ def test_idle_slots_may_hold_anything(K, slots, hkv):
         got.q[i] = 0x7FC0 if i % 2 else 0x7F80
     got.run()
     assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
-    got.check(slots=[0, 1, 2])
+    assert not got.out[1].any() and torch.isneginf(got.lse[1]).all()   # an idle slot: zeros, -inf
+    got.check(slots=[0, 2])
 
 
 def test_pool_past_4_gib(K):
