@@ -1373,14 +1373,14 @@ void build_pack(const kvc_pack* P, const PackInfo& info, unsigned char* img) {
     for (int64_t b = 0, nb = pack_blocks(len, group); b < nb; ++b) {
       const int tiles = pack_tiles(len, group, b);
       if (len <= kvc::kPackShort) {
-        items[ns++] = {(int32_t)row0, len, (int32_t)b, 0, tiles, -1, {0, 0}};
+        items[ns++] = {(int32_t)row0, len, (int32_t)b, 0, tiles, -1, hdr.id};
         continue;
       }
       const int parts = pack_parts(tiles, info.share);
       if (parts > 1) joins[nj++] = {(int32_t)row0, len, (int32_t)b, (int32_t)np, parts, {0, 0, 0}};
       for (int i = 0; i < parts; ++i) {
         const int t0 = (int)((int64_t)tiles * i / parts), t1 = (int)((int64_t)tiles * (i + 1) / parts);
-        items[n++] = {(int32_t)row0, len, (int32_t)b, t0, t1 - t0, parts > 1 ? (int32_t)np++ : -1, {0, 0}};
+        items[n++] = {(int32_t)row0, len, (int32_t)b, t0, t1 - t0, parts > 1 ? (int32_t)np++ : -1, hdr.id};
       }
     }
     row0 += len;

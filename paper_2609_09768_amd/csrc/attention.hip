@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   PackItem item = {};
   if constexpr (PACKED) {
     item = P.items[rest];
-    if (P.plan->id != P.plan_id) return;  // not the plan the call was checked with
+    if (item.id != P.plan_id) return;  // not the plan the call was checked with
   }
   // (of a prefix, blocks of rows run together through the same keys)
   const int split = PACKED ? 0 : PREFIX ? (int)(rest / (unsigned)P.n_blocks) : (int)(rest % (unsigned)P.n_split);
@@ -241,8 +241,10 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   }
   // smallest position among the wave's live queries (tiles at or below it need no mask)
   int pw_min = in_range ? p : INT_MAX;
+  if constexpr (PACKED) pw_min = 32 * sub;  // (of a unit past the last query: nothing is masked, nothing stored)
+  if constexpr (PREFIX) pw_min = (int)n_kv - 1;
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) pw_min = min(pw_min, __shfl_xor(pw_min, m));
+  for (int m = 32; ROWS == Rows::kSelected && m >= 1; m >>= 1) pw_min = min(pw_min, __shfl_xor(pw_min, m));
   pw_min = __builtin_amdgcn_readfirstlane(pw_min);  // equal in every lane: the mask test is scalar
   // this workgroup's share of the block's key tiles (all of them unless split)
   const int n_all = PREFIX ? (int)((n_kv + kBN - 1) / kBN) : (pmax + kBN) / kBN;  // pmax = -1 -> 0 tiles

@@ -222,8 +222,9 @@ struct PackItem {
   int32_t block;         // its units are 8 (4) block and those after it
   int32_t tile0, n_tiles;
   int32_t part;
-  int32_t pad[2];
+  uint64_t id;           // the plan's, so that one load brings both
 };
+static_assert(sizeof(PackItem) == 32, "one 32-byte scalar load");
 // A block whose keys were cut: parts first .. first + n_parts - 1.
 struct PackJoin {
   int32_t row0, len, block, first, n_parts;
