@@ -163,10 +163,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
       qreg[ks] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(qp + ks * 16) : make_uint4(0, 0, 0, 0));
     sees = own ? max(have - P.n_new + (tok - slot * P.n_new) + 1, 0) : P.n_prefix;
   }
-  int sees_least = in ? sees : 0x7fffffff;
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) sees_least = min(sees_least, __shfl_xor(sees_least, m));
-  sees_least = __builtin_amdgcn_readfirstlane(sees_least);
+  in_order();
+  // the block's first row sees the fewest keys: it has the earliest token
+  const int sees_least = own ? max(have - P.n_new + (row0 / P.group - slot * P.n_new) + 1, 0) : P.n_prefix;
 
   // A tile: eight loads of four rows of K, then eight of V; lane l of a load
   // fills 16 bytes at the wave's LDS address + 16 l.  LDS pieces are swizzled
@@ -243,10 +242,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
   const int n = n_all > wave ? (n_all - wave + kWaves - 1) / kWaves : 0;
   auto start = [&](int i) __attribute__((always_inline)) { return i < n ? key0 + kTile * (kWaves * i + wave) : key_end; };
   if (n > 0) {
-    // the queries' loads are done before the count of loads under way begins
-    __builtin_amdgcn_s_waitcnt(wait_vm(0));
-    in_order();
-    issue_k(start(0));
+    issue_k(start(0));  // behind the queries' loads, which are done when the first K tile is
+
     issue_v(start(0));
     for (int i = 0; i < n; ++i) {
       const int k0 = start(i);
