@@ -24,6 +24,9 @@
 // their results.  The matrix work of a tile (v_mfma_f32_32x32x16_bf16: S^T = K
 // Q^T, O^T += V^T P^T, a lane holds one row and 16 of the keys) takes 512
 // cycles, against about 1,500 for a CU's share of HBM to bring its 16 KB.
+// 64 rows of a kv head over 32,256 keys of 8 heads and 300 own rows (149.6 MB)
+// take 45 us with the join, 3.3 TB/s: a share of the prefix is four tiles a wave
+// there, and its first loads and its results count beside them.
 // More rows go to the kernel of the other attentions (attention.hip), whose
 // eight waves of 32 rows share every tile.
 // Scores, softmax and sums are float32 (the sums of the unrounded weights, so
