@@ -368,11 +368,12 @@ kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k
  * key head before the rotation.  Each head x of n_q_heads and n_k_heads first
  * becomes
  *   x / sqrt(mean_e x[e]^2 + eps) * gamma,
- * gamma = gamma_q or gamma_k (device bf16 [D]; one that no head uses may be
- * NULL), eps >= 0 (an all-zero head with eps = 0 gives NaN, as the formula
- * does), and is then rotated; float32 throughout, the angle reduced in
- * float64, rounded once to bfloat16.  Everything else as kvc_qkv_rope; q, k, v
- * must not overlap gamma_q or gamma_k either.
+ * gamma = gamma_q or gamma_k (device bf16 [D]; one that no head uses is not
+ * read and may be NULL), eps >= 0 (an all-zero head with eps = 0 gives NaN, as
+ * the formula does), and is then rotated; float32 throughout, as in
+ * kvc_rms_norm (so a head's squares have to sum to a float32), the angle
+ * reduced in float64, rounded once to bfloat16.  Everything else as
+ * kvc_qkv_rope; q, k, v must not overlap gamma_q or gamma_k either.
  */
 kvc_status kvc_qkv_norm_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads,
                              int32_t n_v_heads, int32_t head_dim, const void* gamma_q, const void* gamma_k,
@@ -491,9 +492,11 @@ kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_b
  * q, out: device bf16 [n_rows, Hq, D]; k, v: device bf16 [n_rows, Hkv, D]; lse:
  * device float32 [n_rows, Hq] or NULL; n_rows at least the sum of the lengths.
  * Rows behind the last sequence are neither read nor written, and no sequence
- * sees what another's rows hold.  softmax_scale 0 means 1/sqrt(D).  bf16 MFMA,
- * float32 scores, softmax and sums; the weights are rounded to bf16 for the
- * product with V.  ws: kvc_packed_attention_workspace bytes (0 for most
+ * sees what another's rows hold, NaN among it; inside a sequence a masked key
+ * has the weight zero, so a v that is not finite spoils earlier rows too.
+ * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
+ * sums; the weights are rounded to bf16 for the product with V.  ws:
+ * kvc_packed_attention_workspace bytes (0 for most
  * batches: few long sequences get their keys cut over several workgroups),
  * 16-byte aligned, KVC_ERR_WORKSPACE below that.  The same call gives the same
  * bits.  Blocks x kv heads of one launch are at most 2^22, a block being eight
@@ -614,13 +617,14 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
  * k_prefix, v_prefix: device bf16 [n_prefix, Hkv, D], e.g. a layer's blended
  * cache (NULL only if n_prefix == 0); k_pages, v_pages: device bf16 [n_pages,
  * page_rows, Hkv, D], one layer's pool.  Rows of a page behind a slot's length
- * may hold anything, NaN among it; rows of a table entry outside [0, n_pages)
- * are left out.  P->ref is not used.  softmax_scale 0 means 1/sqrt(D).  bf16
- * MFMA, float32 scores, softmax and sums; the weights are rounded to bf16 for
- * the product with V.  ws: kvc_shared_prefix_workspace bytes (a part's float32
- * results for each part of the keys, so it grows with max_pages), 16-byte
- * aligned.  The same call gives the same bits.  n_slots x n_new x Hq is at
- * most 2^23.
+ * may hold anything, NaN among it, and so may queries of a slot that is not in
+ * use; rows of a table entry outside [0, n_pages) are left out.  A slot sees
+ * only the prefix, its own pages and its own queries.  P->ref is not used.
+ * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
+ * sums; the weights are rounded to bf16 for the product with V.  ws:
+ * kvc_shared_prefix_workspace bytes (a part's float32 results for each part of
+ * the keys, so it grows with max_pages), 16-byte aligned.  The same call gives
+ * the same bits.  n_slots x n_new x Hq is at most 2^23.
  */
 #define KVC_SHARED_MAX_NEW 4096
 kvc_status kvc_shared_prefix_workspace(const kvc_pages* P, int64_t n_prefix, int32_t n_new,

@@ -886,8 +886,8 @@ static kvc_status qkv_rope_impl(const char* W, const void* y, int64_t n, int32_t
                vb = (size_t)n * n_v_heads * head_dim * 2;
   kvc_status st = check_disjoint(W, {{q, qb, "q"}, {k, kb, "k"}, {v, vb, "v"}},
                                  {{y, yb, "y"}, {pos, (size_t)n * 4, "pos"},
-                                  {norm && n_q_heads > 0 ? norm->gamma_q : nullptr, (size_t)head_dim * 2, "gamma_q"},
-                                  {norm && n_k_heads > 0 ? norm->gamma_k : nullptr, (size_t)head_dim * 2, "gamma_k"}});
+                                  {norm ? norm->gamma_q : nullptr, (size_t)head_dim * 2, "gamma_q"},
+                                  {norm ? norm->gamma_k : nullptr, (size_t)head_dim * 2, "gamma_k"}});
   if (st != KVC_OK) return st;
   st = need_device(W);
   if (st != KVC_OK) return st;
@@ -910,7 +910,9 @@ kvc_status kvc_qkv_norm_rope(const void* y, int64_t n, int32_t n_q_heads, int32_
                              int32_t head_dim, const void* gamma_q, const void* gamma_k, float eps,
                              const int32_t* pos, double rope_theta, const double* inv_freq, void* q, void* k, void* v,
                              void* stream) {
-  const kvc::HeadNorm norm = {static_cast<const uint16_t*>(gamma_q), static_cast<const uint16_t*>(gamma_k), eps};
+  // (weights that no head uses are not read, whatever their pointer is)
+  const kvc::HeadNorm norm = {n_q_heads > 0 ? static_cast<const uint16_t*>(gamma_q) : nullptr,
+                              n_k_heads > 0 ? static_cast<const uint16_t*>(gamma_k) : nullptr, eps};
   return qkv_rope_impl("kvc_qkv_norm_rope", y, n, n_q_heads, n_k_heads, n_v_heads, head_dim, &norm, pos, rope_theta,
                        inv_freq, q, k, v, stream);
 }

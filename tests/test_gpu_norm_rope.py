@@ -76,3 +76,21 @@ def test_values_whose_squares_leave_float32(K):
     torch.cuda.synchronize()
     wq, _ = _want(y, np.arange(6), 1, 0, 0, g, g, 0.0, oracle.inv_freq(128, 500000.0))
     assert _close(down_bf16(q), wq)
+
+
+@pytest.mark.parametrize("hq,hk", [(3, 0), (0, 3), (0, 0)])
+def test_weights_that_no_head_uses_are_not_looked_at(K, hq, hk):
+    # (a pointer of theirs need not be aligned, nor hold 128 weights, nor be apart from the outputs)
+    rng = np.random.default_rng(5)
+    n, hv = 4, 2
+    y = oracle.f64_to_bf16(rng.standard_normal((n, (hq + hk + hv) * 128)))
+    g = oracle.f64_to_bf16(1 + 0.3 * rng.standard_normal(128))
+    q, k, v = (empty_bf16(n, max(h, 1), 128) for h in (hq, hk, hv))
+    other = v.view(-1)[1:]
+    K.kvc_qkv_norm_rope(up(y), n, hq, hk, hv, 128, up(g) if hq else other, up(g) if hk else other, 1e-5, None,
+                        500000.0, q if hq else None, k if hk else None, v)
+    torch.cuda.synchronize()
+    wq, wk = _want(y, np.arange(n), hq, hk, hv, g, g, 1e-5, oracle.inv_freq(128, 500000.0))
+    assert not hq or _close(down_bf16(q), wq)
+    assert not hk or _close(down_bf16(k), wk)
+    assert np.array_equal(down_bf16(v), y.reshape(n, -1, 128)[:, hq + hk:])
