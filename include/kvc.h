@@ -371,9 +371,11 @@ kvc_status kvc_qkv_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k
  * gamma = gamma_q or gamma_k (device bf16 [D]; one that no head uses is not
  * read and may be NULL), eps >= 0 (an all-zero head with eps = 0 gives NaN, as
  * the formula does), and is then rotated; float32 throughout, as in
- * kvc_rms_norm (so a head's squares have to sum to a float32), the angle
- * reduced in float64, rounded once to bfloat16.  Everything else as
- * kvc_qkv_rope; q, k, v must not overlap gamma_q or gamma_k either.
+ * kvc_rms_norm (so a head's squares have to sum to a float32: below root mean
+ * squares of 1e-19, where the squares are subnormal, they lose bits, and at
+ * 1e-23 they are zero), the angle reduced in float64, rounded once to bfloat16.
+ * Everything else as kvc_qkv_rope; q, k, v must not overlap gamma_q or gamma_k
+ * either.
  */
 kvc_status kvc_qkv_norm_rope(const void* y, int64_t n, int32_t n_q_heads, int32_t n_k_heads,
                              int32_t n_v_heads, int32_t head_dim, const void* gamma_q, const void* gamma_k,

@@ -153,10 +153,11 @@ __device__ __forceinline__ float sum8(float x) {
 // The RMS norm of a head of 128 in the registers of the eight lanes that hold
 // it (a: elements 8 jg .., b: 64 + 8 jg .., with the weights ga, gb), in
 // float32, then the rotation of the unrounded values: x' = x / sqrt(mean x^2 +
-// eps) * gamma, rounded once after the rotation.  The hardware's reciprocal
-// root is within one float32 unit.  Bound by HBM like the plain split: 18,856
-// rows of 48 heads take 91 us (5.1 TB/s), the plain split of the same bytes 85
-// to 88 on the same card.
+// eps) * gamma, rounded once after the rotation.  rsqrtf takes a subnormal mean
+// square too (with eps = 0, heads below 1.1e-19), which the bare instruction
+// answers with infinity.  Bound by HBM like the plain split: 18,856 rows of 48
+// heads take 91 us (5.1 TB/s), the plain split of the same bytes 85 to 88 on the
+// same card.
 __device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, const uint4& ga, const uint4& gb,
                                              float eps, const float* c, const float* s, uint4& oa, uint4& ob) {
   float ss = 0.0f;
@@ -166,7 +167,7 @@ __device__ __forceinline__ void norm_rotate8(const uint4& a, const uint4& b, con
     ss = fmaf(x, x, ss);
     ss = fmaf(y, y, ss);
   }
-  const float inv = __builtin_amdgcn_rsqf(sum8(ss) * (1.0f / kHeadDim) + eps);
+  const float inv = rsqrtf(sum8(ss) * (1.0f / kHeadDim) + eps);
   uint32_t ra[4], rb[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
