@@ -653,7 +653,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
           *reinterpret_cast<uint4*>(P.out + ((row0 + r) * P.n_q_heads + h) * (long long)kHeadDim + 8 * (lane & 15)) = line[j];
       }
       if (P.lse && half == 0 && in_range)
-        P.lse[(row0 + qi) * P.n_q_heads + h] = (l_tot > 0.f) ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+        P.lse[(row0 + qi) * P.n_q_heads + h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
       return;
     }
   }
@@ -669,7 +669,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       for (int rr = 0; rr < 4; ++rr)
         po[(dt * 4 + rr) * 64] =
             make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
-    if (half == 0) P.part_lse[at + ql] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+    if (half == 0) P.part_lse[at + ql] = l_tot > 0.f ? m_run + log2f(l_tot) : -INFINITY;
     return;
   }
   if constexpr (PREFIX) {
@@ -681,7 +681,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       for (int rr = 0; rr < 4; ++rr)
         *reinterpret_cast<float4*>(po + dt * 32 + rr * 8) =
             make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
-    if (half == 0) P.part_lse[at] = (l_tot > 0.f) ? m_run + log2f(l_tot) : -INFINITY;
+    if (half == 0) P.part_lse[at] = l_tot > 0.f ? m_run + log2f(l_tot) : -INFINITY;
     return;
   }
   if (P.n_split > 1) {
@@ -853,12 +853,13 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
 #pragma unroll
         for (int r = kb == 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      // (every query sees a key of tile 0, so the maximum is finite from then on)
       const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * P.scale_log2;
       // the offset of the exponents follows the maximum when that has left it by 2^8
       const float m_new = mx2 > m_run + 8.f ? mx2 : m_run;
+      // (every query sees a key of tile 0, but its score may be -inf)
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
       if (__any(m_new != m_run && t > 0)) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -872,8 +873,8 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e], P.scale_log2, -m_new));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e + 1], P.scale_log2, -m_new));
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e], P.scale_log2, -m_use));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kk >> 1][(kk & 1) * 8 + 2 * e + 1], P.scale_log2, -m_use));
           l_run += p0 + p1;
           w[e] = pack_bf16x2(p0, p1);
         }
