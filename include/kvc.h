@@ -26,8 +26,8 @@
  *   *_workspace / *_bytes query returns.
  * - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *   Compute entry points only enqueue work on it and return without waiting.
- *   kvc_plan_upload without a staging buffer is the one exception: it waits
- *   for its own copy.
+ *   kvc_plan_upload and kvc_pack_plan_upload without a staging buffer are the
+ *   exceptions: they wait for their own copy.
  * - Every argument is validated on the host before any HIP call; a bad one
  *   returns KVC_ERR_INVALID_ARG / _UNSUPPORTED / _WORKSPACE and enqueues
  *   nothing.  A HIP failure (including "no device") returns KVC_ERR_DEVICE.
@@ -495,7 +495,8 @@ kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_b
  * device float32 [n_rows, Hq] or NULL; n_rows at least the sum of the lengths.
  * Rows behind the last sequence are neither read nor written, and no sequence
  * sees what another's rows hold, NaN among it; inside a sequence a masked key
- * has the weight zero, so a v that is not finite spoils earlier rows too.
+ * has the weight zero, so a v that is not finite spoils earlier rows too.  A row
+ * with a score of NaN or +inf among those it sees has out and lse NaN.
  * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
  * sums; the weights are rounded to bf16 for the product with V.  ws:
  * kvc_packed_attention_workspace bytes (0 for most
@@ -622,6 +623,10 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
  * may hold anything, NaN among it, and so may queries of a slot that is not in
  * use; rows of a table entry outside [0, n_pages) are left out.  A slot sees
  * only the prefix, its own pages and its own queries.  P->ref is not used.
+ * Inside a slot, own rows behind a query's t have the weight zero for it, so a
+ * value there that is not finite may spoil its out (not its lse): a later draft
+ * token's reaches the earlier ones.  A query with a score of NaN or +inf among
+ * those it sees has out and lse NaN.
  * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
  * sums; the weights are rounded to bf16 for the product with V.  ws:
  * kvc_shared_prefix_workspace bytes (a part's float32 results for each part of

@@ -160,7 +160,9 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
 // kPrefix: rows (token, head of the group) of a kv head that all see every key
 // (a batch over one shared prefix); a unit is 32 of them.
 // In both the weights' sums are taken before they are rounded to bf16, one
-// more addition per pair, which makes the log-sum exact to float32.
+// more addition per pair, which makes the log-sum exact to float32, and a sum
+// of NaN (a query that sees a NaN) stays one: only the sum 0 is a part without
+// keys.
 enum class Rows { kSelected, kPacked, kPrefix };
 template <int UNITS, Rows ROWS = Rows::kSelected>
 __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams P) {
@@ -653,7 +655,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
           *reinterpret_cast<uint4*>(P.out + ((row0 + r) * P.n_q_heads + h) * (long long)kHeadDim + 8 * (lane & 15)) = line[j];
       }
       if (P.lse && half == 0 && in_range)
-        P.lse[(row0 + qi) * P.n_q_heads + h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+        P.lse[(row0 + qi) * P.n_q_heads + h] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * 0.69314718055994531f;
       return;
     }
   }
@@ -669,7 +671,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       for (int rr = 0; rr < 4; ++rr)
         po[(dt * 4 + rr) * 64] =
             make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
-    if (half == 0) P.part_lse[at + ql] = l_tot > 0.f ? m_run + log2f(l_tot) : -INFINITY;
+    if (half == 0) P.part_lse[at + ql] = l_tot == 0.f ? -INFINITY : m_run + log2f(l_tot);
     return;
   }
   if constexpr (PREFIX) {
@@ -681,7 +683,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       for (int rr = 0; rr < 4; ++rr)
         *reinterpret_cast<float4*>(po + dt * 32 + rr * 8) =
             make_float4(o[dt][rr * 4] * inv, o[dt][rr * 4 + 1] * inv, o[dt][rr * 4 + 2] * inv, o[dt][rr * 4 + 3] * inv);
-    if (half == 0) P.part_lse[at] = l_tot > 0.f ? m_run + log2f(l_tot) : -INFINITY;
+    if (half == 0) P.part_lse[at] = l_tot == 0.f ? -INFINITY : m_run + log2f(l_tot);
     return;
   }
   if (P.n_split > 1) {
@@ -856,7 +858,7 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
       const float mx2 = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * P.scale_log2;
       // the offset of the exponents follows the maximum when that has left it by 2^8
       const float m_new = mx2 > m_run + 8.f ? mx2 : m_run;
-      // (every query sees a key of tile 0, but its score may be -inf)
+      // (every query sees a key of tile 0, but its score may be -inf, or NaN)
       const float m_use = m_new == -INFINITY ? 0.f : m_new;
       if (__any(m_new != m_run && t > 0)) {
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
@@ -948,7 +950,7 @@ __global__ __launch_bounds__(64 * kShortWaves, 2) void pack_short_kernel(const A
       __builtin_amdgcn_wave_barrier();
     }
     if (P.lse && half == 0 && qi < cur.len)
-      P.lse[(cur.row0 + qi) * P.n_q_heads + cur.h] = l_tot > 0.f ? (m_run + log2f(l_tot)) * 0.69314718055994531f : -INFINITY;
+      P.lse[(cur.row0 + qi) * P.n_q_heads + cur.h] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * 0.69314718055994531f;
     if (!more) break;
     cur = next;
   }
@@ -1059,7 +1061,7 @@ __global__ __launch_bounds__(kCombineThreads) void pack_join_kernel(const AttnPa
     *reinterpret_cast<uint2*>(op + rr * 8) = make_uint2(pack_bf16x2(a[rr * 4] * inv, a[rr * 4 + 1] * inv),
                                                         pack_bf16x2(a[rr * 4 + 2] * inv, a[rr * 4 + 3] * inv));
   if (P.lse && dt == 0 && half == 0)
-    P.lse[(J.row0 + qi) * P.n_q_heads + h] = wsum > 0.f ? (m + log2f(wsum)) * 0.69314718055994531f : -INFINITY;
+    P.lse[(J.row0 + qi) * P.n_q_heads + h] = wsum == 0.f ? -INFINITY : (m + log2f(wsum)) * 0.69314718055994531f;
 }
 
 hipError_t launch_combine(const AttnParams& P, hipStream_t s) {

@@ -336,6 +336,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
     f[w] = wm[w][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][ql] - m);
     l = fmaf(f[w], wl[w][ql], l);
   }
+  // (a row that sees no key of the part has the sum 0; one with a NaN among its
+  // scores has the sum NaN, whatever its maximum, and keeps it)
   const float inv = l > 0.f ? 1.f / l : 0.f;
   const long long at = ((long long)part * P.n_kv_heads + g) * P.rows + row;
 #pragma unroll
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
             make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
     }
   }
-  if (wave == 0 && half == 0 && in) P.part_lse[at] = l > 0.f ? m + log2f(l) : -INFINITY;
+  if (wave == 0 && half == 0 && in) P.part_lse[at] = l == 0.f ? -INFINITY : m + log2f(l);
 }
 
 // Joins the parts of a row and head with the weights 2^(lse - max), one
@@ -384,13 +386,19 @@ __global__ __launch_bounds__(64 * kJoinWaves) void prefix_join_kernel(const Pref
   const float* op = P.part_o + ((long long)g * P.rows + r) * kHeadDim + 2 * lane;
   float l_first = lane < parts ? lp[lane * stride] : -INFINITY;
   float m = l_first;
-  for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, lp[p * stride]);
+  bool nan = l_first != l_first;  // fmaxf passes over NaN: a row of nothing else is not one without keys
+  for (int p = lane + 64; p < parts; p += 64) {
+    const float l = lp[p * stride];
+    m = fmaxf(m, l);
+    nan |= l != l;
+  }
+  nan = __any(nan);
 #pragma unroll
   for (int x = 32; x >= 1; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
   float a = 0.f, b = 0.f, sum = 0.f;
-  for (int p0 = 0; p0 < parts && m != -INFINITY; p0 += 64) {
+  for (int p0 = 0; p0 < parts && (m != -INFINITY || nan); p0 += 64) {
     const float l = p0 == 0 ? l_first : p0 + lane < parts ? lp[(p0 + lane) * stride] : -INFINITY;
-    const float w = __builtin_amdgcn_exp2f(l - m);  // 0 for a part without keys
+    const float w = __builtin_amdgcn_exp2f(l - m);  // 0 for a part without keys, NaN for one of NaN
     sum += w;
     const int n = min(parts - p0, 64);
     const float* q = op + (long long)p0 * stride * kHeadDim;
@@ -422,7 +430,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void prefix_join_kernel(const Pref
   const float inv = sum > 0.f ? 1.f / sum : 0.f;
   const long long at = (long long)tok * P.n_q_heads + h;
   *reinterpret_cast<uint32_t*>(P.out + at * kHeadDim + 2 * lane) = pack_bf16x2(a * inv, b * inv);
-  if (P.lse && lane == 0) P.lse[at] = sum > 0.f ? (m + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+  if (P.lse && lane == 0) P.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
 }
 
 long long div_up(long long a, long long b) { return (a + b - 1) / b; }

@@ -1,13 +1,131 @@
 """What values that are not finite reach in kvc_packed_attention and
-kvc_shared_prefix_attention."""
+kvc_shared_prefix_attention: a NaN that a query sees makes its output and
+log-sum NaN, and no other query's."""
 import pytest
 import torch
 
 from _attn import attend, bf, check, draw, gen
 from _gpu import dev
 from test_gpu_packed import _run
+from test_gpu_shared_prefix import Case
 
 pytestmark = pytest.mark.gpu
+
+NAN = 0x7FC0
+# short and long blocks, and keys cut over workgroups
+PACKED = [([40, 129, 1, 700], 8, 2), ([900, 1300, 5], 8, 2), ([2048], 4, 1), ([769] * 24, 32, 8)]
+# slots, kv heads of 8 query heads, new tokens: up to 64 rows of a kv head, and more
+SHARED = [(3, 2, 1), (8, 1, 1), (4, 2, 4), (9, 1, 1), (33, 2, 1), (12, 2, 7)]
+
+
+def _nan(x):
+    return bf(x).isnan()
+
+
+# ---------------------------------------------------------------- NaN that a query sees
+@pytest.mark.parametrize("lens,hq,hkv", PACKED)
+def test_packed_nan_query_and_key(K, lens, hq, hkv):
+    g = gen(hq + hkv)
+    n = sum(lens)
+    q, k, v = draw(g, n, hq, 128), draw(g, n, hkv, 128), draw(g, n, hkv, 128)
+    want, want_lse = _run(K, lens, hq, hkv, q, k, v)
+    s = max(range(len(lens)), key=lambda i: lens[i])        # the longest sequence: a query, then a key of it
+    lo, row = sum(lens[:s]), lens[s] * 2 // 3
+    q2 = q.clone()
+    q2[lo + row, hq - 1, 5] = NAN
+    out, lse = _run(K, lens, hq, hkv, q2, k, v)
+    hit = torch.zeros((n, hq), dtype=torch.bool, device=dev())
+    hit[lo + row, hq - 1] = True
+    assert _nan(out)[hit].all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+    k2 = k.clone()
+    k2[lo + row, hkv - 1, 77] = NAN
+    out, lse = _run(K, lens, hq, hkv, q, k2, v)
+    hit.zero_()
+    hit[lo + row:lo + lens[s], hq - hq // hkv:] = True
+    assert _nan(out)[hit].all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
+def _same_but(c, want, hit):
+    """hit: [slots, new, query heads], the rows that are NaN; the others have the bits of the case without it."""
+    assert _nan(c.out)[hit].all() and c.lse[hit].isnan().all()
+    assert torch.equal(c.out[~hit], want.out[~hit]) and torch.equal(c.lse[~hit], want.lse[~hit])
+
+
+@pytest.mark.parametrize("slots,hkv,n_new", SHARED)
+@pytest.mark.parametrize("n_prefix", [0, 2, 3001])
+def test_shared_nan_query_and_key(K, slots, hkv, n_new, n_prefix):
+    lens = [n_new + 61 * i % 700 for i in range(slots)]
+    lens[slots // 2] = 0                                     # an idle slot
+    make = lambda: Case(K, n_prefix, lens, n_new, 8, hkv, 16, seed=slots + n_prefix)  # noqa: E731
+    want = make().run()
+    live = torch.zeros((slots, n_new, 8), dtype=torch.bool, device=dev())
+    for s, x in enumerate(lens):
+        live[s] = x > 0
+    none = torch.zeros_like(live)
+    grp = slice(8 - 8 // hkv, 8)                             # the query heads of the last kv head
+    # a query
+    c, hit = make(), none.clone()
+    c.q[slots - 1, n_new - 1, 7, 64] = NAN
+    hit[slots - 1, n_new - 1, 7] = True
+    _same_but(c.run(), want, hit)
+    # a key of the prefix: every query of its head that is in use
+    if n_prefix:
+        for row in {0, n_prefix - 1, n_prefix // 2}:
+            c = make()
+            c.kp[row, hkv - 1, 127] = NAN
+            hit = none.clone()
+            hit[:, :, grp] = live[:, :, grp]
+            _same_but(c.run(), want, hit)
+    # an own key: the slot's queries from its row on
+    s = slots - 1
+    for back in {0, n_new - 1, min(n_new, lens[s] - 1)}:
+        c, row = make(), lens[s] - 1 - back
+        c.k[int(c.table[s, row // 16]), row % 16, hkv - 1, 3] = NAN
+        hit = none.clone()
+        hit[s, max(n_new - 1 - back, 0):, grp] = True
+        _same_but(c.run(), want, hit)
+
+
+def test_scores_that_leave_float32(K):
+    # a score of +inf, like a NaN: the softmax of it is none
+    g = gen(3)
+    q, k, v = draw(g, 100, 4, 128), draw(g, 100, 2, 128), draw(g, 100, 2, 128)
+    q[:, :, 0], k[:, :, 0] = 0, 0
+    want, want_lse = _run(K, [100], 4, 2, q, k, v)
+    q[60, 3, 0], k[20, 1, 0] = 0x7F00, 0x7F00                # 2^127 each
+    hit = torch.zeros((100, 4), dtype=torch.bool, device=dev())
+    hit[60, 3] = True
+    out, lse = _run(K, [100], 4, 2, q, k, v)
+    assert _nan(out)[hit].all() and lse[hit].isnan().all()
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+    for slots in (4, 40):
+        make = lambda: Case(K, 900, [5 + i for i in range(slots)], 1, 8, 2, 16, seed=slots)  # noqa: E731
+        want = make()
+        want.q[:, :, :, 0] = 0
+        want.kp[:, :, 0] = 0
+        want.run()
+        c = make()
+        c.q[:, :, :, 0] = 0
+        c.kp[:, :, 0] = 0
+        c.q[1, 0, 2, 0], c.kp[333, 0, 0] = 0x7F00, 0x7F00
+        hit = torch.zeros((slots, 1, 8), dtype=torch.bool, device=dev())
+        hit[1, 0, 2] = True
+        _same_but(c.run(), want, hit)
+
+
+@pytest.mark.parametrize("slots", [3, 40])
+def test_values_that_are_not_finite_reach_their_own_slot_only(K, slots):
+    # a later draft token's infinite value has weight zero for earlier ones of its slot, and may spoil them; no other
+    lens = [20 + 3 * i for i in range(slots)]
+    make = lambda: Case(K, 200, lens, 4, 8, 2, 16, seed=7)  # noqa: E731
+    want, c = make().run(), make()
+    row = lens[1] - 1
+    c.v[int(c.table[1, row // 16]), row % 16] = 0x7F80
+    c.run()
+    rest = [s for s in range(slots) if s != 1]
+    assert torch.equal(c.out[rest], want.out[rest]) and torch.equal(c.lse, want.lse)
 
 
 def test_keys_whose_scores_are_all_infinitely_negative(K):
