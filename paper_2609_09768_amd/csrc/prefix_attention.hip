@@ -29,10 +29,13 @@
 // there, and its first loads and its results count beside them.
 // More rows go to the kernel of the other attentions (attention.hip), whose
 // eight waves of 32 rows share every tile.
-// Scores, softmax and sums are float32 (the sums of the unrounded weights, so
-// the log-sum is exact to float32); weights are rounded to bf16 for the product
-// with V, whose operand they are: each is off by 2^-8 of itself at most, and
-// the output is rounded to as many bits.
+// Scores, softmax and sums are float32; weights are rounded to bf16 for the
+// product with V, whose operand they are: each is off by 2^-8 of itself at most,
+// and the output is rounded to as many bits.  A part's output is divided by the
+// sum of its rounded weights, which makes it a weighted mean of V (over the
+// unrounded sum a row that one key dominates is off by that key's rounding, up
+// to 0.38 %); the log-sum, the part's weight in the join, takes the sum of the
+// unrounded ones and is exact to float32.
 #include <algorithm>
 
 #include "bf16_util.h"
@@ -105,7 +108,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
   // a part of each for every wave
   __shared__ __attribute__((aligned(16))) uint16_t Ks[kWaves * kKSlot];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[kWaves * kVSlot];
-  __shared__ float wm[kWaves][32], wl[kWaves][32];
+  __shared__ float wm[kWaves][32], wl[kWaves][32], wu[kWaves][32];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -231,7 +234,8 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
   }
 
   f32x16 o[4];
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = -INFINITY, l_run = 0.f, u_run = 0.f;  // sums of the weights as rounded to bf16, and before that
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -286,6 +290,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
       if (__any(m_new != m_run)) {
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
         l_run *= alpha;
+        u_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -296,8 +301,9 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float p0 = __builtin_amdgcn_exp2f(s[2 * e] - m_use), p1 = __builtin_amdgcn_exp2f(s[2 * e + 1] - m_use);
-        l_run += p0 + p1;
+        u_run += p0 + p1;
         w[e] = pack_bf16x2(p0, p1);
+        l_run = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), ones, l_run, false);
       }
       const bf16x8 pb[2] = {as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])), as_bf16x8(make_uint4(w[4], w[5], w[6], w[7]))};
       __builtin_amdgcn_s_waitcnt(wait_vm(8));  // V
@@ -321,20 +327,22 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
   // join the waves, 32 channels at a time (16 KB of LDS), in wave order
   float4* const red = reinterpret_cast<float4*>(Ks);
   static_assert(sizeof(Ks) >= kWaves * 4 * 64 * sizeof(float4), "the waves' sums of a quarter of the channels");
-  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  const float l_tot = l_run + __shfl_xor(l_run, 32), u_tot = u_run + __shfl_xor(u_run, 32);
   if (half == 0) {
     wm[wave][ql] = m_run;
     wl[wave][ql] = l_tot;
+    wu[wave][ql] = u_tot;
   }
   __syncthreads();  // all waves are done with their slots
   float m = -INFINITY;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) m = fmaxf(m, wm[w][ql]);
-  float l = 0.f, f[kWaves];
+  float l = 0.f, u = 0.f, f[kWaves];
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     f[w] = wm[w][ql] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(wm[w][ql] - m);
     l = fmaf(f[w], wl[w][ql], l);
+    u = fmaf(f[w], wu[w][ql], u);
   }
   // (a row that sees no key of the part has the sum 0; one with a NaN among its
   // scores has the sum NaN, whatever its maximum, and keeps it)
@@ -362,7 +370,7 @@ __global__ __launch_bounds__(kThreads, 2) void prefix_attn_kernel(const PrefixPa
             make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
     }
   }
-  if (wave == 0 && half == 0 && in) P.part_lse[at] = l == 0.f ? -INFINITY : m + log2f(l);
+  if (wave == 0 && half == 0 && in) P.part_lse[at] = u == 0.f ? -INFINITY : m + log2f(u);
 }
 
 // Joins the parts of a row and head with the weights 2^(lse - max), one

@@ -1,6 +1,8 @@
-"""What values that are not finite reach in kvc_packed_attention and
-kvc_shared_prefix_attention: a NaN that a query sees makes its output and
-log-sum NaN, and no other query's."""
+"""What values reach in kvc_packed_attention and kvc_shared_prefix_attention: a
+NaN that a query sees makes its output and log-sum NaN, and no other query's;
+an output is a weighted mean of V."""
+import math
+
 import pytest
 import torch
 
@@ -144,3 +146,51 @@ def test_keys_whose_scores_are_all_infinitely_negative(K):
     for h in (0, 1):
         want = attend(bf(q[:, h]), bf(k[:, 0]), bf(v[:, 0]), torch.arange(1, 201, device=dev()))
         check(out[:, h], lse[:, h], want)
+
+
+# ---------------------------------------------------------------- a mean of V
+# An output is a weighted mean of V.  A row whose values are all equal has that value as its output, whatever its weights: they are rounded to bf16
+# for the product with V, and so have to be the ones whose sum it is divided by.  The float32 sums of up to 4,000
+# weights and of their products with one value are off by less than 2^-12 of themselves each; 1.9921875 is 2^-9
+# from the next value's border, relative to itself, so the bits are the same.
+SAME = 0x3FFF
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.0, 0.3])
+@pytest.mark.parametrize("lens,hq,hkv", PACKED)
+def test_packed_output_of_equal_values(K, lens, hq, hkv, scale):
+    g = gen(len(lens) + hq)
+    n = sum(lens)
+    q, k = draw(g, n, hq, 128, scale=1.5), draw(g, n, hkv, 128, scale=1.5)
+    v = torch.full((n, hkv, 128), SAME, dtype=torch.int16, device=dev())
+    out, _ = _run(K, lens, hq, hkv, q, k, v, scale)
+    assert (out == SAME).all(), int((out != SAME).sum())
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.0, 0.3])
+@pytest.mark.parametrize("slots,hkv,n_new", SHARED)
+@pytest.mark.parametrize("n_prefix", [0, 700, 3001])
+def test_shared_output_of_equal_values(K, slots, hkv, n_new, n_prefix, scale):
+    c = Case(K, n_prefix, [n_new + 37 * i % 600 for i in range(slots)], n_new, 8, hkv, 16, seed=slots)
+    c.vp.fill_(SAME)
+    c.v.masked_fill_(c.v != NAN, SAME)          # (rows that no slot holds stay NaN)
+    c.run(scale)
+    assert (c.out == SAME).all(), int((c.out != SAME).sum())
+
+
+@pytest.mark.parametrize("slots,n_new", [(2, 1), (2, 40)])
+def test_shared_output_of_one_dominant_key(K, slots, n_new):
+    # own rows of which one has nearly all of the weight, 129.45 times that of an earlier one: between two bf16 values,
+    # and too little more for the offset of the exponents to follow
+    c = Case(K, 0, [200] * slots, n_new, 8, 1, 16, seed=1)
+    c.q.fill_(0)
+    c.q[..., 0] = 0x3F80                                     # 1
+    c.v.masked_fill_(c.v != NAN, SAME)
+    for s in range(slots):
+        for row in range(200):
+            a = {3: 0.0, 130: 1.0}.get(row, -8.0)
+            c.k[int(c.table[s, row // 16]), row % 16] = 0
+            c.k[int(c.table[s, row // 16]), row % 16, 0, 0] = torch.tensor(a).to(torch.bfloat16).view(torch.int16).item()
+    c.run(math.log(129.45))
+    assert (c.out == SAME).all()
+    assert (c.lse - math.log(130.45)).abs().max() < 2.0 ** -18 * 5   # d of tests/_attn.py
