@@ -1307,7 +1307,8 @@ kvc_status check_pack(const char* W, const kvc_pack* P, PackInfo* info) {
   if (st != KVC_OK) return st;
   const int group = P->n_q_heads / P->n_kv_heads;
   PackInfo i;
-  int64_t twice = 0;  // tiles of all blocks, twice: blocks x (first + last block's tiles)
+  int64_t twice = 0;   // tiles of all blocks, twice: blocks x (first + last block's tiles)
+  int64_t blocks = 0;  // of eight units, whatever the kernel's own are: the limit that kvc.h states
   int longest = 0;
   for (int32_t s = 0; s < P->n_seqs; ++s) {
     const int32_t len = P->seq_len[s];
@@ -1319,12 +1320,14 @@ kvc_status check_pack(const char* W, const kvc_pack* P, PackInfo* info) {
     const int tiles = pack_tiles(len, group, n - 1);
     const bool is_short = len <= kvc::kPackShort;
     (is_short ? i.n_short : i.n_items) += n;
+    blocks += ((len + int64_t(31)) / 32 * group + kvc::kPackUnits - 1) / kvc::kPackUnits;
     twice += n * (pack_tiles(len, group, 0) + tiles) / (is_short ? 2 : 1);
     if (!is_short) longest = std::max(longest, tiles);
   }
   // one launch: fewer than 2^32 work-items, cut blocks included (those are
-  // cut only where there are few, see pack_parts)
-  if ((i.n_items + i.n_short) * P->n_kv_heads > (int64_t(1) << 22))
+  // cut only where there are few, see pack_parts); short sequences' blocks, at
+  // most twice as many, are a plan's items and no workgroups
+  if (blocks * P->n_kv_heads > (int64_t(1) << 22))
     return fail(KVC_ERR_INVALID_ARG, "%s: too many queries and heads for one launch", W);
   i.share = (twice * P->n_kv_heads + 2 * kCus - 1) / (2 * kCus);
   if (pack_parts(longest, i.share) > 1)
