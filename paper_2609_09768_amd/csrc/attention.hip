@@ -61,7 +61,7 @@
 //   than 768 rows (16 of 7,750 rows of 32/8 heads 7.6 ms, 1.04 PFLOP/s; a block
 //   of 61 tiles costs about 9 us beside them, and the board's power holds the
 //   tiles to 1.8 us) and a batch's rows over a shared prefix (256 rows of a kv
-//   head over 124,256 keys of 8 heads 121 us: 130 GFLOP at 1.08 PFLOP/s, 4.2
+//   head over 124,256 keys of 8 heads 123 us: 130 GFLOP at 1.06 PFLOP/s, 4.1
 //   TB/s).  Shorter packed sequences have a kernel of their own below.
 
 #include "kvc_internal.h"
@@ -741,10 +741,10 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 // tiles are asked for beside the last two of the present one and its queries
 // beside the output, and one workgroup's waits lie beside the other's products.
 // Tiles go through two slots and a plain loop.  32,000 rows of documents of 16 to
-// 512 (32/8 heads) take 193 us, 3.4 TB/s of the bytes that have to move; with one
-// sum of the weights instead of two it was 190, and of those 167 without the
-// products, 147 without the queries' loads, 157 without the output, so the
-// strided 256-byte heads bound it.
+// 512 (32/8 heads) take 193 us (190 with one sum of the weights instead of two).
+// 659 MB have to move and 837 do, 4.3 TB/s: 272 written, and 565 read in
+// 128-byte requests where queries, keys and values are 393, so a good part of the
+// keys comes from memory more than once.
 constexpr int kShortWaves = 4;
 static_assert(kShortWaves == kPackShortUnits && kWaves == kPackUnits, "the plan's blocks");
 constexpr int kShortRow = 40;  // bf16 between rows of 32 channels on their way out
