@@ -499,7 +499,7 @@ kvc_status kvc_pack_plan_upload(const kvc_pack* P, void* plan_dev, size_t plan_b
  * with a score of NaN or +inf among those it sees has out and lse NaN.
  * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
  * sums; the weights are rounded to bf16 for the product with V, and out is
- * divided by the sum of the rounded ones (a weighted mean of V).  ws:
+ * divided by their sum as rounded where they count (a weighted mean of V).  ws:
  * kvc_packed_attention_workspace bytes (0 for most
  * batches: few long sequences get their keys cut over several workgroups),
  * 16-byte aligned, KVC_ERR_WORKSPACE below that.  The same call gives the same
@@ -630,7 +630,7 @@ kvc_status kvc_pages_copy(const kvc_pages* P, const int32_t* src, const int32_t*
  * those it sees has out and lse NaN.
  * softmax_scale 0 means 1/sqrt(D).  bf16 MFMA, float32 scores, softmax and
  * sums; the weights are rounded to bf16 for the product with V, and out is
- * divided by the sum of the rounded ones (a weighted mean of V).  ws:
+ * divided by their sum as rounded where they count (a weighted mean of V).  ws:
  * kvc_shared_prefix_workspace bytes (a part's float32 results for each part of
  * the keys, so it grows with max_pages), 16-byte aligned.  The same call gives
  * the same bits.  n_slots x n_new x Hq is at most 2^23.

@@ -58,9 +58,9 @@
 //   workspace for their float32 partial outputs and LSEs); a second kernel
 //   merges the partials of each unit in split order.
 // - The same pipeline runs causal attention inside packed sequences of more
-//   than 768 rows (16 of 7,750 rows of 32/8 heads 7.6 ms, 1.04 PFLOP/s; a block
+//   than 768 rows (16 of 7,750 rows of 32/8 heads 7.4 ms, 1.07 PFLOP/s; a block
 //   of 61 tiles costs about 9 us beside them, and the board's power holds the
-//   tiles to 1.8 us) and a batch's rows over a shared prefix (256 rows of a kv
+//   tiles to 1.75 us) and a batch's rows over a shared prefix (256 rows of a kv
 //   head over 124,256 keys of 8 heads 123 us: 130 GFLOP at 1.06 PFLOP/s, 4.1
 //   TB/s).  Shorter packed sequences have a kernel of their own below.
 
@@ -99,6 +99,12 @@ constexpr unsigned kLoadMask2 = 0x0000u;
 constexpr int kWaitVm8 = 8 | (7 << 4);
 constexpr int kWaitVm4 = 4 | (7 << 4);
 constexpr float kSumLimit = 65536.0f;     // bound on a lane's tile sum of weights (32 of them)
+// Of packed sequences and prefixes: a lane's tile whose weights are more than
+// this share of its sum before counts into the divisor as rounded.  Times of
+// 1/4 and 1/8 differ by less than two runs of one; for normal scores of a spread
+// from 1 to 8 and for rows of 2 to 10 heavy keys (on the host) the divisor is then
+// within 0.04 % of the rounded weights' sum, 0.08 % at 1/4, 0.35 % with no such tile.
+constexpr float kHeavyTile = 0.125f;
 
 struct AttnParams {
   const uint16_t* q;
@@ -159,13 +165,15 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
 // of the key tiles come from the plan's work items; the rest is the same.
 // kPrefix: rows (token, head of the group) of a kv head that all see every key
 // (a batch over one shared prefix); a unit is 32 of them.
-// In both the weights are also summed before they are rounded to bf16 (lu, two
-// more additions per pair), which makes the log-sum exact to float32.  The
-// output is divided by the sum of the rounded ones, as everywhere: a weighted
-// mean of V, where the other sum leaves a row that one key dominates off by that
-// key's rounding, up to 0.38 % (with the one sum 7.2 ms instead of 7.6 in the case
-// above).  A sum of NaN (a query that sees a NaN) stays one: only the sum 0 is a
-// part without keys.
+// In both the weights are summed before they are rounded to bf16 (one more
+// addition per pair), which makes the log-sum exact to float32.  That sum would
+// leave the output of a row that one key dominates off by that key's rounding, up
+// to 0.38 %; the divisor is a sum of its own, which takes a tile's weights as
+// rounded where they are much of it (kHeavyTile; few tiles behind the first
+// dozen), so that the output is a weighted mean of V as everywhere.  16 sequences of
+// 7,750 rows of 32/8 heads take 7.38 ms so, 7.23 with the one sum, 7.56 with
+// both sums over every tile.  A sum of NaN (a query that sees a NaN) stays one:
+// only the sum 0 is a part without keys.
 enum class Rows { kSelected, kPacked, kPrefix };
 template <int UNITS, Rows ROWS = Rows::kSelected>
 __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams P) {
@@ -296,20 +304,15 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   auto load_part = [&](int t, uint16_t* ks_, uint16_t* vs_, int q) __attribute__((always_inline)) {
     const int tile = t0 + t;
     const long long r0 = (long long)tile * kBN;
-    const int j = q & 1;
-    // (with the sums of two kinds there is no register for a second offset: its
-    // four rows move the base and leave the rows that are left)
-    constexpr bool kFold = ROWS != Rows::kSelected;
-    const int skip = kFold ? 4 * j : 0, at = kFold ? 0 : j;
-    int rows = tile < n_full ? kBN : (tile == n_full ? n_tail : 0);
-    if constexpr (kFold) rows = max(rows - skip, 0);
+    const int rows = tile < n_full ? kBN : (tile == n_full ? n_tail : 0);
     const int nbytes = rows * (int)row_bytes;
+    const int j = q & 1;
     if (q < 2) {
-      const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + (r0 + skip) * row_bytes), (short)0, nbytes, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (2 * wave + j) * kKGroup), 16, koff[at], 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(kbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(ks_ + (2 * wave + j) * kKGroup), 16, koff[j], 0, 0, 0);
     } else {
-      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + (r0 + skip) * row_bytes), (short)0, nbytes, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (8 * wave + 4 * j) * kHeadDim), 16, voff[at], 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vbase + r0 * row_bytes), (short)0, nbytes, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(vs_ + (8 * wave + 4 * j) * kHeadDim), 16, voff[j], 0, 0, 0);
     }
   };
   auto load_tile = [&](int t, uint16_t* ks_, uint16_t* vs_) __attribute__((always_inline)) {
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   float m_run = -INFINITY;
   float m_use = 0.f;
   float l_run = 0.f;        // this lane's partial sum (its 16 keys of each 32)
-  float u_run = 0.f;        // the same before rounding (packed sequences and prefixes)
+  float u_run = 0.f;        // of packed sequences and prefixes: the unrounded weights, for the log-sum
   f32x16 o[4];
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -397,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = key0 + kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          s[kb][r] = key > (PREFIX ? pw_min : p) ? -INFINITY : s[kb][r];
+          s[kb][r] = key > p ? -INFINITY : s[kb][r];
         }
     }
   };
@@ -415,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   // Weights of half a tile (keys 32*hf .. 32*hf+31, accumulator s[hf]) as
   // the bf16 B operands of two 16-key PV steps; the tile sum adds those same
   // bf16 weights.
-  auto exp_half = [&](const f32x16* s, auto hfc, bf16x8* pb2, float& lt, float& lu) __attribute__((always_inline)) {
+  auto exp_half = [&](const f32x16* s, auto hfc, bf16x8* pb2, float& lt) __attribute__((always_inline)) {
     constexpr int hf = decltype(hfc)::value;
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
@@ -426,8 +429,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
         const float p1 = __builtin_amdgcn_exp2f(fmaf(s[hf][k2 * 8 + 2 * e + 1], c2, -m_use));
         const f32x2 pv2 = {p0, p1};
         const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-        if constexpr (ROWS != Rows::kSelected) lu += p0 + p1;
-        lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
+        if constexpr (ROWS != Rows::kSelected) lt += p0 + p1;
+        else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
         w[e] = __builtin_bit_cast(uint32_t, pw);
       }
       pb2[k2] = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
@@ -443,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   // tile is taken again.  Other queries keep their offset and get the same
   // weights again, so a query's result does not depend on the other
   // queries of its wave.
-  auto redo = [&](const f32x16* s, bf16x8* pl, bf16x8* ph, float& lt, float& lu, bool bad) __attribute__((always_inline)) {
+  auto redo = [&](const f32x16* s, bf16x8* pl, bf16x8* ph, float& lt, bool bad) __attribute__((always_inline)) {
     const float mt = tile_max(s);
     const auto sw = __builtin_amdgcn_permlane32_swap((uint32_t)bad, (uint32_t)bad, false, false);
     const bool bad_q = (sw[0] | sw[1]) != 0u;
@@ -457,10 +460,9 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
     m_run = m_new;
     m_use = (m_run == -INFINITY) ? 0.f : m_run;
-    if constexpr (ROWS != Rows::kSelected) m_run = m_use;
-    lt = lu = 0.f;
-    exp_half(s, H0{}, pl, lt, lu);
-    exp_half(s, H1{}, ph, lt, lu);
+    lt = 0.f;
+    exp_half(s, H0{}, pl, lt);
+    exp_half(s, H1{}, ph, lt);
   };
   // O^T += V^T P^T for a V^T tile, 16 keys per step (steps 0, 1 from the
   // tile's first half, 2, 3 from its second)
@@ -472,13 +474,13 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     }
   };
   // The two phases of a pipeline step.  Each issues 16 MFMAs of one product
-  // and, between them, the 48 VALU instructions (64 with the second sum) that
-  // turn half a tile of scores into weights: every MFMA is followed by the LDS
-  // read for the MFMA two places later and by three or four VALU instructions
-  // (one weight pair per two MFMAs: exponent FMAs, exponentials, bf16 pack,
-  // sums) that run two places ahead, so the first of them cover the latency of
-  // the first LDS reads.  The groups are fenced so the compiler keeps this order.
-  auto exp_part = [&](const f32x16* se, int hf, int i, float& p0, float& x1, uint32_t (&w)[2][4], float& lt, float& lu)
+  // and, between them, the 48 VALU instructions that turn half a tile of
+  // scores into weights (56 where their sum is unrounded): every MFMA is followed
+  // by the LDS read for the MFMA two places later and by three VALU instructions
+  // (one weight pair per two MFMAs: exponent FMAs, exponentials, bf16 pack, sum)
+  // that run two places ahead, so the first of them cover the latency of the
+  // first LDS reads.  The groups are fenced so the compiler keeps this order.
+  auto exp_part = [&](const f32x16* se, int hf, int i, float& p0, float& x1, uint32_t (&w)[2][4], float& lt)
       __attribute__((always_inline)) {
     const int j = i >> 1, k2 = j >> 2, e = j & 3;
     if ((i & 1) == 0) {
@@ -488,15 +490,15 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       const float p1 = __builtin_amdgcn_exp2f(x1);
       const f32x2 pv2 = {p0, p1};
       const bf16x2 pw = __builtin_convertvector(pv2, bf16x2);
-      if constexpr (ROWS != Rows::kSelected) lu += p0 + p1;
-      lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
+      if constexpr (ROWS != Rows::kSelected) lt += p0 + p1;
+      else lt = __builtin_amdgcn_fdot2_f32_bf16(pw, ones, lt, false);
       w[k2][e] = __builtin_bit_cast(uint32_t, pw);
     }
   };
   // phase 1: S^T of the next tile (K tile ks_) beside the weights of the
   // second half of the current tile (scores se); its last two slots read
   // the first two V^T fragments of phase 2 (tile vt_) into fv.
-  auto phase1 = [&](const uint16_t* ks_, f32x16* sq, const f32x16* se, bf16x8* ph, float& lt, float& lu,
+  auto phase1 = [&](const uint16_t* ks_, f32x16* sq, const f32x16* se, bf16x8* ph, float& lt,
                     const uint16_t* vt_, uint4 (&fv)[2], auto&& after) __attribute__((always_inline)) {
     uint4 fr[3];
     float p0 = 0.f, x1 = 0.f;
@@ -504,8 +506,8 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     fr[0] = k_frag(ks_, 0);
     fr[1] = k_frag(ks_, 1);
     __builtin_amdgcn_sched_barrier(0);
-    exp_part(se, 1, 0, p0, x1, w, lt, lu);
-    exp_part(se, 1, 1, p0, x1, w, lt, lu);
+    exp_part(se, 1, 0, p0, x1, w, lt);
+    exp_part(se, 1, 1, p0, x1, w, lt);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -513,7 +515,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
       else fv[i - 14] = v_frag(vt_, i - 14);
       const int kb = i >> 3, ks = i & 7;
       sq[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fr[i % 3]), qreg[ks], ks == 0 ? f32x16{} : sq[kb], 0, 0, 0);
-      if (i + 2 < 16) exp_part(se, 1, i + 2, p0, x1, w, lt, lu);
+      if (i + 2 < 16) exp_part(se, 1, i + 2, p0, x1, w, lt);
       after(i);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -524,21 +526,21 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   // ph; first two fragments already in fv) beside the weights of the first
   // half of the next tile (scores se)
   auto phase2 = [&](const uint16_t* vt_, const uint4 (&fv)[2], const bf16x8* pl, const bf16x8* ph,
-                    const f32x16* se, bf16x8* pn, float& lt, float& lu, auto&& after) __attribute__((always_inline)) {
+                    const f32x16* se, bf16x8* pn, float& lt, auto&& after) __attribute__((always_inline)) {
     uint4 fr[3];
     float p0 = 0.f, x1 = 0.f;
     uint32_t w[2][4];
     fr[0] = fv[0];
     fr[1] = fv[1];
-    exp_part(se, 0, 0, p0, x1, w, lt, lu);
-    exp_part(se, 0, 1, p0, x1, w, lt, lu);
+    exp_part(se, 0, 0, p0, x1, w, lt);
+    exp_part(se, 0, 1, p0, x1, w, lt);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i + 2 < 16) fr[(i + 2) % 3] = v_frag(vt_, i + 2);
       const int kk = i >> 2, dt = i & 3;
       o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fr[i % 3]), kk < 2 ? pl[kk] : ph[kk - 2], o[dt], 0, 0, 0);
-      if (i + 2 < 16) exp_part(se, 0, i + 2, p0, x1, w, lt, lu);
+      if (i + 2 < 16) exp_part(se, 0, i + 2, p0, x1, w, lt);
       after(i);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -567,13 +569,30 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   // a fence would also wait for the loads of tile t+3.
   f32x16 s[2][2];
   bf16x8 pbl[2][2], pbh[2];
-  float lt[2] = {0.f, 0.f}, lu[2] = {0.f, 0.f};
+  float lt[2] = {0.f, 0.f};
   auto check = [&](auto parc) __attribute__((always_inline)) {
     constexpr int PA = decltype(parc)::value;
     const bool bad = !(lt[PA] <= kSumLimit);
-    if (__any(bad)) redo(s[PA], pbl[PA], pbh, lt[PA], lu[PA], bad);
-    l_run += lt[PA];
-    if constexpr (ROWS != Rows::kSelected) u_run += lu[PA];
+    if (__any(bad)) redo(s[PA], pbl[PA], pbh, lt[PA], bad);
+    if constexpr (ROWS == Rows::kSelected) {
+      l_run += lt[PA];
+    } else {
+      const bool heavy = lt[PA] > kHeavyTile * l_run;
+      float add = lt[PA];
+      if (__any(heavy)) {
+        float r = 0.f;
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const uint4 a = __builtin_bit_cast(uint4, pbl[PA][k2]), b = __builtin_bit_cast(uint4, pbh[k2]);
+          const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) r = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), ones, r, false);
+        }
+        if (heavy) add = r;
+      }
+      l_run += add;
+      u_run += lt[PA];
+    }
   };
   auto step = [&](auto slotc, auto parc, int t) __attribute__((always_inline)) {
     constexpr int B0 = decltype(slotc)::value;
@@ -583,13 +602,13 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     // loads of tile t+3, spread over phase 1 (the last tile may load again; harmless)
     const int tl = min(t + 3, n_tiles - 1);
     uint4 fv[2];
-    phase1(Ks[B1], s[1 - PA], s[PA], pbh, lt[PA], lu[PA], Vs[B0], fv, [&](int i) __attribute__((always_inline)) {
+    phase1(Ks[B1], s[1 - PA], s[PA], pbh, lt[PA], Vs[B0], fv, [&](int i) __attribute__((always_inline)) {
       if (kLoadMask1 >> i & 1) load_part(tl, Ks[B3], Vs[B3], __builtin_popcount(kLoadMask1 & ((1u << i) - 1)));
     });
     check(parc);
     mask(t + 1, s[1 - PA]);
-    lt[1 - PA] = lu[1 - PA] = 0.f;
-    phase2(Vs[B0], fv, pbl[PA], pbh, s[1 - PA], pbl[1 - PA], lt[1 - PA], lu[1 - PA], [&](int i) __attribute__((always_inline)) {
+    lt[1 - PA] = 0.f;
+    phase2(Vs[B0], fv, pbl[PA], pbh, s[1 - PA], pbl[1 - PA], lt[1 - PA], [&](int i) __attribute__((always_inline)) {
       if (kLoadMask2 >> i & 1) load_part(tl, Ks[B3], Vs[B3], __builtin_popcount(kLoadMask1) + __builtin_popcount(kLoadMask2 & ((1u << i) - 1)));
     });
     __builtin_amdgcn_s_waitcnt(kWaitVm4);
@@ -598,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
   auto last = [&](auto slotc, auto parc, int t) __attribute__((always_inline)) {
     constexpr int B0 = decltype(slotc)::value;
     constexpr int PA = decltype(parc)::value;
-    exp_half(s[PA], H1{}, pbh, lt[PA], lu[PA]);
+    exp_half(s[PA], H1{}, pbh, lt[PA]);
     check(parc);
     pv(pbl[PA], pbh, Vs[B0]);
   };
@@ -614,8 +633,7 @@ __global__ __launch_bounds__(kThreads) void sparse_attn_kernel(const AttnParams 
     mask(0, s[0]);
     m_run = tile_max(s[0]);
     m_use = (m_run == -INFINITY) ? 0.f : m_run;
-    if constexpr (ROWS != Rows::kSelected) m_run = m_use;  // (one register: a row without keys is known by its sum)
-    exp_half(s[0], H0{}, pbl[0], lt[0], lu[0]);
+    exp_half(s[0], H0{}, pbl[0], lt[0]);
     __builtin_amdgcn_s_waitcnt(kWaitVm4);  // tile 1
     __builtin_amdgcn_s_barrier();
     int t = 0;

@@ -149,10 +149,11 @@ def test_keys_whose_scores_are_all_infinitely_negative(K):
 
 
 # ---------------------------------------------------------------- a mean of V
-# An output is a weighted mean of V.  A row whose values are all equal has that value as its output, whatever its weights: they are rounded to bf16
-# for the product with V, and so have to be the ones whose sum it is divided by.  The float32 sums of up to 4,000
-# weights and of their products with one value are off by less than 2^-12 of themselves each; 1.9921875 is 2^-9
-# from the next value's border, relative to itself, so the bits are the same.
+# An output is a weighted mean of V.  A row whose values are all equal has that value as its output, whatever its
+# weights: they are rounded to bf16 for the product with V, and so have to be the ones whose sum it is divided by (the
+# long kernels' divisor is within 2^-11 of that).  The float32 sums of up to 4,000 weights and of their products with
+# one value are off by less than 2^-12 of themselves each; 1.9921875 is 2^-9 from the next value's border, relative to
+# itself, so the bits are the same.
 SAME = 0x3FFF
 
 
